@@ -380,6 +380,115 @@ gm_status gm_hyper_bwd(const float* dlogits, const float* z, const float* gru, f
 gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64_t n, double lr, double beta1,
                    double beta2, double eps, double weight_decay, int32_t step, gm_stream_t stream);
 
+/*
+ * Low-rank adapters beside a target linear.  What pruning costs is won back by
+ * tuning a low-rank update beside the frozen masked weight, and one pruned
+ * model serves the updates of many requests at once.  A pool holds n adapters
+ * of one rank r for a stack of `parts` projections that read the same input
+ * (q|k|v or gate|up side by side, as the packed linear has them; parts = 1 for
+ * one projection), with output widths widths[0] + .. = d_out:
+ *   A [n, parts r, d_in] bf16, part k's ranks at rows k r .. (k + 1) r - 1;
+ *   B [n, d_out, r] bf16; scale [n] fp32 (4-byte aligned).
+ * Token t has adapter a = adapter[t], none if that is outside 0 .. n - 1
+ * (-1, say).  With its c = scale[a]:
+ *   P[t] = X[t] A_a^T                                        [T, parts r]
+ *   Y[t, part k] = base[t, part k] + c P[t, ranks of k] B_a[part k]^T
+ *   Q[t, ranks of k] = c dY[t, part k] B_a[part k]
+ *   dX[t] = base[t] + Q[t] A_a
+ *   dA_a = sum over a's tokens of Q[t]^T X[t]
+ *   dB_a[part k] = c sum over a's tokens of dY[t, part k]^T P[t, ranks of k]
+ * Rows of tokens without an adapter are base's own in Y and dX, and zero in P.
+ * An adapter that no token has gets zero gradients.  Products accumulate in
+ * fp32; P, Q, dA and dB stay fp32 (in Y and dX, c P and Q enter with 16 bits of
+ * significand; in dA and dB with all 24); Y and dX are rounded once.  Values
+ * of a token or of its adapter that are not finite make its rows (and that
+ * adapter's gradients) not finite, and no others.  Results do not
+ * depend on timing, and a token's Y and P not on the order of the batch.
+ *   1 <= T <= 262144; 1 <= n <= 2048; r a multiple of 8 in [8, 128];
+ *   1 <= parts <= 4; d_in and every width multiples of 8, d_in and d_out at
+ *   most 2^18.  widths is a HOST array.  X, dY, base, Y and dX have a row
+ *   stride in elements (ldx ...), a multiple of 8 and at least the row's length,
+ *   so that they may be columns of wider buffers; base may be Y (dX) itself
+ *   with the same stride, else it must not overlap it.  All but `adapter`
+ *   (4-byte aligned) and scale are 16-byte aligned.
+ *
+ * gm_lora_plan_size, gm_lora_workspace_size (op GM_OP_FWD or GM_OP_BWD) --
+ * host-only queries of the bytes that the calls below need.
+ */
+#define GM_LORA_MAX_PARTS 4
+gm_status gm_lora_plan_size(int64_t T, int32_t n, size_t* bytes);
+gm_status gm_lora_workspace_size(int op, int64_t T, int32_t n, int64_t d_in, const int64_t* widths, int32_t parts,
+                                 int32_t r, size_t* bytes);
+
+/*
+ * gm_lora_plan -- sorts the tokens of a batch by adapter (stably): one launch
+ * per batch, whose plan all linears of the model share, forward and backward.
+ *   adapter [T] int32; plan: plan_bytes >= gm_lora_plan_size(T, n), caller-owned;
+ *   only the calls below read it.  A plan that was made for another T or n is
+ *   not followed: they then write nothing.
+ */
+gm_status gm_lora_plan(const int32_t* adapter, int64_t T, int32_t n, void* plan, size_t plan_bytes,
+                       gm_stream_t stream);
+
+/*
+ * gm_lora_fwd -- Y [T, d_out] bf16, written in full, and P [T, parts r] fp32
+ * where it is not NULL (gm_lora_bwd takes it).  ws: caller-owned scratch.
+ */
+gm_status gm_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, const float* scale,
+                      const void* plan, size_t plan_bytes, int64_t T, int32_t n, int64_t d_in, const int64_t* widths,
+                      int32_t parts, int32_t r, const uint16_t* base, int64_t ld_base, uint16_t* Y, int64_t ldy,
+                      float* P, void* ws, size_t ws_bytes, gm_stream_t stream);
+
+/*
+ * gm_lora_bwd -- dX [T, d_in] bf16, dA [n, parts r, d_in] and
+ * dB [n, d_out, r] fp32, each written in full or NULL to skip it (all three
+ * NULL is a no-op).  P is the forward's (needed for dB only), base the gradient
+ * that dX adds to (needed for dX only; the dX of gm_masked_linear_bwd).
+ */
+gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64_t ldx, const uint16_t* A,
+                      const uint16_t* B, const float* scale, const void* plan, size_t plan_bytes, const float* P,
+                      int64_t T, int32_t n, int64_t d_in, const int64_t* widths, int32_t parts, int32_t r,
+                      const uint16_t* base, int64_t ld_base, uint16_t* dX, int64_t lddx, float* dA, float* dB,
+                      void* ws, size_t ws_bytes, gm_stream_t stream);
+
+/*
+ * Lists of tensors, for the optimiser's work over many of them in one call.
+ * gm_tensor_list writes a list (caller-owned, at least gm_tensor_list_size
+ * bytes, 16-byte aligned) of n tensors of numel[i] values: gradients g[i], and unless p is
+ * NULL parameters p[i] with moments m[i] and v[i], all fp32, and unless p16 is NULL a bf16 copy
+ * p16[i] of the parameters.  g[i] is bf16 where g_bf16 (may be NULL) is not 0, else fp32.
+ * All these arrays are HOST arrays (read before the call returns) of DEVICE
+ * pointers, which need their element's alignment only; tensors that are
+ * all 16-byte aligned (p16: 8) go faster.  The list holds the addresses, not
+ * the values: it stays good while the buffers live, and the calls below that
+ * take it need it ordered before them on their stream.
+ *   1 <= n <= 65536; numel[i] >= 0 (pointers of empty tensors may be NULL).
+ */
+gm_status gm_tensor_list_size(const int64_t* numel, int32_t n, size_t* bytes);
+gm_status gm_tensor_list(float* const* p, const void* const* g, float* const* m, float* const* v,
+                         uint16_t* const* p16, const uint8_t* g_bf16, const int64_t* numel, int32_t n, void* list,
+                         size_t list_bytes, gm_stream_t stream);
+
+/*
+ * gm_grad_norm -- norm = sqrt(sum of the squares of every gradient of the
+ * list) and coef = min(1, max_norm / norm), one fp32 each (device).  The sum is
+ * in fp64 and in a fixed order.  A norm that is not finite gives coef = 0.
+ *   max_norm > 0 (infinity: coef is 1); ws: GM_GRAD_NORM_WORKSPACE_BYTES of scratch.
+ */
+#define GM_GRAD_NORM_WORKSPACE_BYTES ((size_t)16384)
+gm_status gm_grad_norm(const void* list, size_t list_bytes, float max_norm, float* norm, float* coef, void* ws,
+                       size_t ws_bytes, gm_stream_t stream);
+
+/*
+ * gm_adamw_list -- one gm_adamw step on every tensor of the list with the gradients coef g
+ * (coef: one fp32 (device), or NULL for 1), and the bf16 copies of the new
+ * parameters.  The gradients themselves stay as they are.  With coef = 0, as
+ * gm_grad_norm gives it for gradients that are not finite, nothing is changed.
+ * A list without parameters is a no-op.
+ */
+gm_status gm_adamw_list(const void* list, size_t list_bytes, double lr, double beta1, double beta2, double eps,
+                        double weight_decay, int32_t step, const float* coef, gm_stream_t stream);
+
 #ifdef __cplusplus
 } /* extern "C" */
 #endif

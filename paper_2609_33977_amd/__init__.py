@@ -10,4 +10,6 @@ from ._lib import (  # noqa: F401
     gm_pack_rows, gm_packed_linear_fwd,
     gm_distill_workspace_size, gm_distill_fwd, gm_distill_bwd,
     gm_hyper_workspace_size, gm_hyper_fwd, gm_hyper_bwd, gm_adamw,
+    GM_LORA_MAX_PARTS, gm_lora_plan_size, gm_lora_workspace_size, gm_lora_plan, gm_lora_fwd, gm_lora_bwd,
+    GM_GRAD_NORM_WORKSPACE_BYTES, gm_tensor_list_size, gm_tensor_list, gm_grad_norm, gm_adamw_list,
 )

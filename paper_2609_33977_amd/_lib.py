@@ -26,6 +26,8 @@ EXPORTS = (
     "gm_masked_linear_fwd", "gm_masked_linear_bwd", "gm_masked_linear_bwd_noalloc", "gm_pack_rows", "gm_packed_linear_fwd",
     "gm_distill_workspace_size", "gm_distill_fwd", "gm_distill_bwd",
     "gm_hyper_workspace_size", "gm_hyper_fwd", "gm_hyper_bwd", "gm_adamw",
+    "gm_lora_plan_size", "gm_lora_workspace_size", "gm_lora_plan", "gm_lora_fwd", "gm_lora_bwd",
+    "gm_tensor_list_size", "gm_tensor_list", "gm_grad_norm", "gm_adamw_list",
 )
 
 
@@ -66,6 +68,17 @@ def _load() -> ctypes.CDLL:
         "gm_hyper_bwd": ([P, P, P, P, P, P, P, P, P, I64, I64, I64, I64, F64, F64, F64, F64, F64, I32, P, P, SZ, P],
                          ctypes.c_int),
         "gm_adamw": ([P, P, P, P, I64, F64, F64, F64, F64, F64, I32, P], ctypes.c_int),
+        "gm_lora_plan_size": ([I64, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "gm_lora_workspace_size": ([ctypes.c_int, I64, I32, I64, P, I32, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "gm_lora_plan": ([P, I64, I32, P, SZ, P], ctypes.c_int),
+        "gm_lora_fwd": ([P, I64, P, P, P, P, SZ, I64, I32, I64, P, I32, I32, P, I64, P, I64, P, P, SZ, P],
+                        ctypes.c_int),
+        "gm_lora_bwd": ([P, I64, P, I64, P, P, P, P, SZ, P, I64, I32, I64, P, I32, I32, P, I64, P, I64, P, P, P, SZ, P],
+                        ctypes.c_int),
+        "gm_tensor_list_size": ([P, I32, ctypes.POINTER(SZ)], ctypes.c_int),
+        "gm_tensor_list": ([P, P, P, P, P, P, P, I32, P, SZ, P], ctypes.c_int),
+        "gm_grad_norm": ([P, SZ, F32, P, P, P, SZ, P], ctypes.c_int),
+        "gm_adamw_list": ([P, SZ, F64, F64, F64, F64, F64, I32, P, P], ctypes.c_int),
     }
     for name, (args, res) in sigs.items():
         fn = getattr(lib, name)
@@ -372,3 +385,202 @@ def gm_adamw(p, g, m, v, lr: float, beta1: float, beta2: float, eps: float, weig
         _arg("gm_adamw", what, t, "f32", numel=n)
     _check(LIB.gm_adamw(_ptr(p), _ptr(g), _ptr(m), _ptr(v), p.numel(), float(lr), float(beta1), float(beta2),
                         float(eps), float(weight_decay), int(step), _stream(stream)), "gm_adamw")
+
+
+# ---- low-rank adapters beside a masked or packed linear
+
+GM_LORA_MAX_PARTS = 4
+
+
+def _rows(where, what, t, cols, rows):
+    """Pointer and row stride of a bf16 matrix that may be columns of a wider one."""
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{where}: {what} must be {torch.bfloat16}, got {t.dtype}")
+    have = t.shape
+    if len(have) != 2 or have[0] != rows or have[1] != cols:
+        raise ValueError(f"{where}: {what} must have shape {(rows, cols)}, got {tuple(have)}")
+    ld, one = t.stride()
+    if rows == 1 or ld == 0:  # one row's stride means nothing; rows that share memory are no matrix
+        if rows > 1:
+            raise ValueError(f"{where}: {what} repeats one row")
+        ld = cols
+    if one != 1 and cols > 1:
+        raise ValueError(f"{where}: {what} must have contiguous rows")
+    if not t.is_cuda:
+        raise ValueError(f"{where}: {what} must live on the GPU")
+    return t.data_ptr(), ld
+
+
+def _one_device(where, *tensors):
+    """The kernels run on the current device: every tensor has to be there."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{where}: every tensor must live on the current device {dev}, got one on {t.device}")
+
+
+_WIDTHS = {}  # the C arrays of the few width lists that a model has
+
+
+def _widths(where, widths, d_out):
+    widths = (d_out,) if widths is None else tuple(widths)
+    if sum(widths) != d_out or not 1 <= len(widths) <= GM_LORA_MAX_PARTS:
+        raise ValueError(f"{where}: widths {widths} must be 1 to {GM_LORA_MAX_PARTS} parts of d_out = {d_out}")
+    got = _WIDTHS.get(widths)
+    if got is None:
+        if len(_WIDTHS) > 4096:
+            _WIDTHS.clear()
+        got = _WIDTHS[widths] = (ctypes.c_int64 * len(widths))(*widths)
+    return got
+
+
+def gm_lora_plan_size(T: int, n: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(LIB.gm_lora_plan_size(int(T), int(n), ctypes.byref(out)), "gm_lora_plan_size")
+    return out.value
+
+
+def gm_lora_workspace_size(op: int, T: int, n: int, d_in: int, widths, r: int) -> int:
+    """widths: the output width, or the widths of the stacked projections."""
+    widths = (int(widths),) if isinstance(widths, int) else tuple(int(w) for w in widths)
+    w = (ctypes.c_int64 * max(len(widths), 1))(*widths)
+    out = ctypes.c_size_t(0)
+    _check(LIB.gm_lora_workspace_size(int(op), int(T), int(n), int(d_in), w, len(widths), int(r), ctypes.byref(out)),
+           "gm_lora_workspace_size")
+    return out.value
+
+
+def gm_lora_plan(adapter, n: int, plan, stream=None) -> None:
+    """Sorts the tokens of a batch by adapter (see gm_lora_plan in the header); adapter [T] int32."""
+    w = "gm_lora_plan"
+    _arg(w, "adapter", adapter, "i32", shape=(None,))
+    _arg(w, "plan", plan, "u8")
+    a, p = _ptr(adapter), _ptr(plan)
+    _one_device(w, adapter, plan)
+    _check(LIB.gm_lora_plan(a, adapter.shape[0], int(n), p, plan.numel(), _stream(stream)), w)
+
+
+def _adapters(w, A, B, scale, widths):
+    """(n, d_in, d_out, parts, r, C array of widths) of a pool."""
+    _arg(w, "A", A, "bf16", shape=(None, None, None))
+    n, R, d_in = A.shape
+    _arg(w, "B", B, "bf16", shape=(n, None, None))
+    d_out, r = B.shape[1], B.shape[2]
+    parts = _widths(w, widths, d_out)
+    if R != len(parts) * r:
+        raise ValueError(f"{w}: A must hold {len(parts)} x {r} ranks, got {R}")
+    _arg(w, "scale", scale, "f32", numel=n)
+    return n, R, d_in, d_out, r, parts
+
+
+def gm_lora_fwd(X, A, B, scale, plan, base, Y, P=None, ws=None, widths=None, stream=None) -> None:
+    """Y = base + the adapters' update of every token, and P for the backward (see gm_lora_fwd in the header).
+
+    X, base and Y may be columns of wider buffers; widths are those of stacked projections (None: one)."""
+    w = "gm_lora_fwd"
+    n, R, d_in, d_out, r, parts = _adapters(w, A, B, scale, widths)
+    T = X.shape[0]
+    _arg(w, "P", P, "f32", shape=(T, R), optional=True)
+    _arg(w, "plan", plan, "u8")
+    _arg(w, "ws", ws, "u8")
+    x, ldx = _rows(w, "X", X, d_in, T)
+    b, ldb = _rows(w, "base", base, d_out, T)
+    y, ldy = _rows(w, "Y", Y, d_out, T)
+    _one_device(w, X, A, B, scale, plan, base, Y, P, ws)
+    _check(LIB.gm_lora_fwd(x, ldx, _ptr(A), _ptr(B), _ptr(scale), _ptr(plan), plan.numel(), T, n, d_in, parts,
+                           len(parts), r, b, ldb, y, ldy, _ptr(P), _ptr(ws), ws.numel(), _stream(stream)), w)
+
+
+def gm_lora_bwd(dY, X, A, B, scale, plan, P, base=None, dX=None, dA=None, dB=None, ws=None, widths=None,
+                stream=None) -> None:
+    """Gradients of the adapters and of their input (see gm_lora_bwd in the header); P, base only as the outputs need."""
+    w = "gm_lora_bwd"
+    n, R, d_in, d_out, r, parts = _adapters(w, A, B, scale, widths)
+    T = X.shape[0]
+    _arg(w, "P", P, "f32", shape=(T, R), optional=dB is None)
+    _arg(w, "dA", dA, "f32", shape=(n, R, d_in), optional=True)
+    _arg(w, "dB", dB, "f32", shape=(n, d_out, r), optional=True)
+    _arg(w, "plan", plan, "u8")
+    _arg(w, "ws", ws, "u8")
+    y, ldy = _rows(w, "dY", dY, d_out, T)
+    x, ldx = _rows(w, "X", X, d_in, T)
+    b = dx = None
+    ldb = lddx = d_in
+    if dX is not None:
+        if base is None:
+            raise ValueError(f"{w}: base is required")
+        b, ldb = _rows(w, "base", base, d_in, T)
+        dx, lddx = _rows(w, "dX", dX, d_in, T)
+    _one_device(w, dY, X, A, B, scale, plan, P, base, dX, dA, dB, ws)
+    _check(LIB.gm_lora_bwd(y, ldy, x, ldx, _ptr(A), _ptr(B), _ptr(scale), _ptr(plan), plan.numel(), _ptr(P), T, n,
+                           d_in, parts, len(parts), r, b, ldb, dx, lddx, _ptr(dA), _ptr(dB), _ptr(ws), ws.numel(),
+                           _stream(stream)), w)
+
+
+# ---- the optimiser's work over lists of tensors
+
+GM_GRAD_NORM_WORKSPACE_BYTES = 16384
+
+
+def gm_tensor_list_size(numels) -> int:
+    numels = list(numels)
+    out = ctypes.c_size_t(0)
+    _check(LIB.gm_tensor_list_size((ctypes.c_int64 * max(len(numels), 1))(*numels), len(numels), ctypes.byref(out)),
+           "gm_tensor_list_size")
+    return out.value
+
+
+def gm_tensor_list(g, list, p=None, m=None, v=None, p16=None, stream=None) -> None:
+    """Writes the addresses of many tensors into `list` (see gm_tensor_list in the header).
+
+    g: their gradients, fp32 or bf16 each; p, m, v: parameters and moments (fp32); p16: bf16 copies of the parameters.
+    The caller keeps the tensors alive for as long as the list is used."""
+    w = "gm_tensor_list"
+    g = tuple(g)
+    n = len(g)
+    rest = {}
+    for what, ts, dtype in (("p", p, torch.float32), ("m", m, torch.float32), ("v", v, torch.float32),
+                            ("p16", p16, torch.bfloat16)):
+        if ts is not None:
+            rest[what] = ts = tuple(ts)
+            if len(ts) != n:
+                raise ValueError(f"{w}: {what} must hold {n} tensors, got {len(ts)}")
+            for t, s in zip(ts, g):
+                if t.dtype is not dtype or t.numel() != s.numel():
+                    raise ValueError(f"{w}: every {what} must be {dtype} of its gradient's size")
+    for t in g:
+        if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
+            raise ValueError(f"{w}: gradients must be {torch.float32} or {torch.bfloat16}, got {t.dtype}")
+    _arg(w, "list", list, "u8")
+    _one_device(w, list, *g, *(t for ts in rest.values() for t in ts))
+
+    def array(ts):
+        return None if ts is None else (ctypes.c_void_p * max(n, 1))(*(_ptr(t) if t.numel() else None for t in ts))
+
+    numel = (ctypes.c_int64 * max(n, 1))(*(t.numel() for t in g))
+    b16 = (ctypes.c_uint8 * max(n, 1))(*(t.dtype is torch.bfloat16 for t in g))
+    _check(LIB.gm_tensor_list(array(rest.get("p")), array(g), array(rest.get("m")), array(rest.get("v")),
+                              array(rest.get("p16")), b16, numel, n, _ptr(list), list.numel(), _stream(stream)), w)
+
+
+def gm_grad_norm(list, max_norm: float, norm, coef, ws, stream=None) -> None:
+    """The norm of all gradients of a list, and the coefficient that clips it to max_norm (both fp32, on the device)."""
+    w = "gm_grad_norm"
+    _arg(w, "list", list, "u8")
+    _arg(w, "norm", norm, "f32", numel=1)
+    _arg(w, "coef", coef, "f32", numel=1)
+    _arg(w, "ws", ws, "u8")
+    _one_device(w, list, norm, coef, ws)
+    _check(LIB.gm_grad_norm(_ptr(list), list.numel(), float(max_norm), _ptr(norm), _ptr(coef), _ptr(ws), ws.numel(),
+                            _stream(stream)), w)
+
+
+def gm_adamw_list(list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, coef=None,
+                  stream=None) -> None:
+    """One AdamW step on every tensor of a list with the gradients coef g (coef None: 1)."""
+    w = "gm_adamw_list"
+    _arg(w, "list", list, "u8")
+    _arg(w, "coef", coef, "f32", numel=1, optional=True)
+    _one_device(w, list, coef)
+    _check(LIB.gm_adamw_list(_ptr(list), list.numel(), float(lr), float(beta1), float(beta2), float(eps),
+                             float(weight_decay), int(step), _ptr(coef), _stream(stream)), w)

@@ -12,6 +12,7 @@
 
 #include "../../include/groupmask.h"
 #include "gm_launch.h"
+#include "gm_list.h"
 
 #define GM_EXPORT extern "C" __attribute__((visibility("default")))
 
@@ -270,6 +271,74 @@ gm::HyperWs hyper_ws(void* ws, const HyperLayout& Y) {
   w.dgi = reinterpret_cast<float*>(b + Y.dgi);
   w.dgh = reinterpret_cast<float*>(b + Y.dgh);
   return w;
+}
+
+// Low-rank adapters.  Rows and columns are indexed with 32-bit ints, rows of
+// the tall matrices and the adapters of a pool with 64-bit offsets.
+constexpr int64_t kMaxLoraTokens = 262144;
+constexpr int32_t kMaxAdapters = 2048;
+constexpr int64_t kMaxLoraDim = int64_t(1) << 18;
+constexpr int32_t kMaxRank = 128;
+
+gm_status check_lora_batch(int64_t T, int32_t n) {
+  return T < 1 || T > kMaxLoraTokens || n < 1 || n > kMaxAdapters ? GM_ERR_SHAPE : GM_OK;
+}
+
+gm_status check_lora_shape(int64_t T, int32_t n, int64_t d_in, const int64_t* widths, int32_t parts, int32_t r,
+                           gm::LoraShape* z) {
+  if (gm_status st = check_lora_batch(T, n)) return st;
+  if (!widths) return GM_ERR_NULL;
+  if (d_in < 8 || d_in > kMaxLoraDim || d_in % 8) return GM_ERR_SHAPE;
+  if (parts < 1 || parts > gm::kLoraMaxParts) return GM_ERR_SHAPE;
+  if (r < 8 || r > kMaxRank || r % 8) return GM_ERR_SHAPE;
+  *z = gm::LoraShape{int(T), int(n), int(d_in), 0, int(parts), int(r), {}};
+  int64_t d_out = 0;
+  for (int p = 0; p < parts; ++p) {
+    if (widths[p] < 8 || widths[p] > kMaxLoraDim || widths[p] % 8) return GM_ERR_SHAPE;
+    z->widths[p] = int(widths[p]);
+    d_out += widths[p];
+  }
+  if (d_out > kMaxLoraDim) return GM_ERR_SHAPE;
+  z->d_out = int(d_out);
+  return GM_OK;
+}
+
+// Rows of a tall matrix: 16-byte vectors at every row's start.
+bool lora_rows_ok(int64_t ld, int64_t cols) { return ld >= cols && ld % 8 == 0 && ld <= (int64_t(1) << 32); }
+
+int lora_fwd_splits(const gm::LoraShape& z) {
+  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles, z.d_in);
+}
+int lora_bwd_splits(const gm::LoraShape& z) {
+  int widest = 0;
+  for (int p = 0; p < z.parts; ++p) widest = std::max(widest, z.widths[p]);
+  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles * z.parts, widest);
+}
+
+// Workspace of the adapters' backward, each part 256-byte aligned (see gm::LoraBwdWs).
+struct LoraBwdLayout {
+  size_t part, Q, partA, partB, total;
+};
+
+LoraBwdLayout lora_bwd_layout(const gm::LoraShape& z) {
+  LoraBwdLayout Y;
+  const size_t low = size_t(z.T) * z.parts * z.r * sizeof(float);
+  const size_t g = size_t(gm::lora_plan_layout(z.T, z.n).max_gtiles);
+  size_t off = 0;
+  auto take = [&](size_t& at, size_t bytes) {
+    at = off;
+    off = round_up(off + bytes, 256);
+  };
+  take(Y.part, size_t(lora_bwd_splits(z)) * low);
+  take(Y.Q, low);
+  take(Y.partA, g * z.parts * z.r * z.d_in * sizeof(float));
+  take(Y.partB, g * z.d_out * z.r * sizeof(float));
+  Y.total = off;
+  return Y;
+}
+
+size_t lora_fwd_workspace(const gm::LoraShape& z) {
+  return round_up(size_t(lora_fwd_splits(z)) * z.T * z.parts * z.r * sizeof(float), 256);
 }
 
 }  // namespace
@@ -598,4 +667,148 @@ GM_EXPORT gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64
   if (n == 0) return GM_OK;
   if (gm_status st = check_device()) return st;
   return from_hip(gm::launch_adamw(p, g, m, v, n, lr, beta1, beta2, eps, weight_decay, step, stream));
+}
+
+GM_EXPORT gm_status gm_lora_plan_size(int64_t T, int32_t n, size_t* bytes) {
+  if (!bytes) return GM_ERR_NULL;
+  if (gm_status st = check_lora_batch(T, n)) return st;
+  *bytes = gm::lora_plan_layout(T, n).words * 4;
+  return GM_OK;
+}
+
+GM_EXPORT gm_status gm_lora_plan(const int32_t* adapter, int64_t T, int32_t n, void* plan, size_t plan_bytes,
+                                 gm_stream_t stream) {
+  if (!adapter || !plan) return GM_ERR_NULL;
+  if (gm_status st = check_lora_batch(T, n)) return st;
+  if (!aligned4(adapter) || !aligned16(plan)) return GM_ERR_ALIGN;
+  if (plan_bytes < gm::lora_plan_layout(T, n).words * 4) return GM_ERR_WORKSPACE;
+  if (gm_status st = check_device()) return st;
+  return from_hip(gm::launch_lora_plan(adapter, int(T), int(n), plan, stream));
+}
+
+GM_EXPORT gm_status gm_lora_workspace_size(int op, int64_t T, int32_t n, int64_t d_in, const int64_t* widths,
+                                           int32_t parts, int32_t r, size_t* bytes) {
+  if (!bytes) return GM_ERR_NULL;
+  if (op != GM_OP_FWD && op != GM_OP_BWD) return GM_ERR_VALUE;
+  gm::LoraShape z;
+  if (gm_status st = check_lora_shape(T, n, d_in, widths, parts, r, &z)) return st;
+  *bytes = op == GM_OP_FWD ? lora_fwd_workspace(z) : lora_bwd_layout(z).total;
+  return GM_OK;
+}
+
+GM_EXPORT gm_status gm_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B,
+                                const float* scale, const void* plan, size_t plan_bytes, int64_t T, int32_t n,
+                                int64_t d_in, const int64_t* widths, int32_t parts, int32_t r, const uint16_t* base,
+                                int64_t ld_base, uint16_t* Y, int64_t ldy, float* P, void* ws, size_t ws_bytes,
+                                gm_stream_t stream) {
+  if (!X || !A || !B || !scale || !plan || !base || !Y) return GM_ERR_NULL;
+  gm::LoraShape z;
+  if (gm_status st = check_lora_shape(T, n, d_in, widths, parts, r, &z)) return st;
+  if (!lora_rows_ok(ldx, d_in) || !lora_rows_ok(ld_base, z.d_out) || !lora_rows_ok(ldy, z.d_out)) return GM_ERR_SHAPE;
+  if (base == Y && ld_base != ldy) return GM_ERR_SHAPE;
+  if (!aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned4(scale) || !aligned16(plan) || !aligned16(base) ||
+      !aligned16(Y) || (P && !aligned16(P)))
+    return GM_ERR_ALIGN;
+  if (plan_bytes < gm::lora_plan_layout(T, n).words * 4) return GM_ERR_WORKSPACE;
+  if (!ws || ws_bytes < lora_fwd_workspace(z)) return GM_ERR_WORKSPACE;
+  if (!aligned16(ws)) return GM_ERR_ALIGN;
+  if (gm_status st = check_device()) return st;
+  return from_hip(gm::launch_lora_fwd(X, ldx, A, B, scale, plan, z, base, ld_base, Y, ldy, P, static_cast<float*>(ws),
+                                      lora_fwd_splits(z), stream));
+}
+
+GM_EXPORT gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64_t ldx, const uint16_t* A,
+                                const uint16_t* B, const float* scale, const void* plan, size_t plan_bytes,
+                                const float* P, int64_t T, int32_t n, int64_t d_in, const int64_t* widths,
+                                int32_t parts, int32_t r, const uint16_t* base, int64_t ld_base, uint16_t* dX,
+                                int64_t lddx, float* dA, float* dB, void* ws, size_t ws_bytes, gm_stream_t stream) {
+  if (!dY || !X || !A || !B || !scale || !plan) return GM_ERR_NULL;
+  if ((dX && !base) || (dB && !P)) return GM_ERR_NULL;
+  gm::LoraShape z;
+  if (gm_status st = check_lora_shape(T, n, d_in, widths, parts, r, &z)) return st;
+  if (!lora_rows_ok(lddy, z.d_out) || !lora_rows_ok(ldx, d_in)) return GM_ERR_SHAPE;
+  if (dX && (!lora_rows_ok(ld_base, d_in) || !lora_rows_ok(lddx, d_in) || (base == dX && ld_base != lddx)))
+    return GM_ERR_SHAPE;
+  if (!aligned16(dY) || !aligned16(X) || !aligned16(A) || !aligned16(B) || !aligned4(scale) || !aligned16(plan) ||
+      (dX && (!aligned16(base) || !aligned16(dX))) || (P && !aligned16(P)) || (dA && !aligned16(dA)) ||
+      (dB && !aligned16(dB)))
+    return GM_ERR_ALIGN;
+  if (plan_bytes < gm::lora_plan_layout(T, n).words * 4) return GM_ERR_WORKSPACE;
+  if (!dX && !dA && !dB) return GM_OK;
+  const LoraBwdLayout Y = lora_bwd_layout(z);
+  if (!ws || ws_bytes < Y.total) return GM_ERR_WORKSPACE;
+  if (!aligned16(ws)) return GM_ERR_ALIGN;
+  if (gm_status st = check_device()) return st;
+  char* b = static_cast<char*>(ws);
+  auto f = [&](size_t off) { return reinterpret_cast<float*>(b + off); };
+  const gm::LoraBwdWs w = {f(Y.part), f(Y.Q), f(Y.partA), f(Y.partB)};
+  return from_hip(gm::launch_lora_bwd(dY, lddy, X, ldx, A, B, scale, plan, P, z, base, ld_base, dX, lddx, dA, dB, w,
+                                      lora_bwd_splits(z), stream));
+}
+
+namespace {
+
+gm_status list_size(const int64_t* numel, int32_t n, size_t* bytes) {
+  if (!numel) return GM_ERR_NULL;
+  if (n < 1 || n > 65536) return GM_ERR_SHAPE;
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (numel[i] < 0 || numel[i] > (int64_t(1) << 40)) return GM_ERR_SHAPE;
+    chunks += gm::list_chunks(numel[i]);
+    if (chunks > (int64_t(1) << 30)) return GM_ERR_SHAPE;
+  }
+  *bytes = gm::list_bytes_of(n, chunks);
+  return GM_OK;
+}
+
+}  // namespace
+
+GM_EXPORT gm_status gm_tensor_list_size(const int64_t* numel, int32_t n, size_t* bytes) {
+  if (!bytes) return GM_ERR_NULL;
+  return list_size(numel, n, bytes);
+}
+
+GM_EXPORT gm_status gm_tensor_list(float* const* p, const void* const* g, float* const* m, float* const* v,
+                                   uint16_t* const* p16, const uint8_t* g_bf16, const int64_t* numel, int32_t n,
+                                   void* list, size_t list_bytes, gm_stream_t stream) {
+  if (!g || !list) return GM_ERR_NULL;
+  if (!p != !m || !p != !v || (p16 && !p)) return GM_ERR_NULL;
+  size_t need = 0;
+  if (gm_status st = list_size(numel, n, &need)) return st;
+  for (int32_t i = 0; i < n; ++i) {
+    if (numel[i] == 0) continue;
+    if (!g[i] || (p && (!p[i] || !m[i] || !v[i])) || (p16 && !p16[i])) return GM_ERR_NULL;
+    const uintptr_t ga = g_bf16 && g_bf16[i] ? 2 : 4;
+    if ((reinterpret_cast<uintptr_t>(g[i]) & (ga - 1)) != 0) return GM_ERR_ALIGN;
+    if (p && (!aligned4(p[i]) || !aligned4(m[i]) || !aligned4(v[i]))) return GM_ERR_ALIGN;
+    if (p16 && (reinterpret_cast<uintptr_t>(p16[i]) & 1) != 0) return GM_ERR_ALIGN;
+  }
+  if (!aligned16(list)) return GM_ERR_ALIGN;
+  if (list_bytes < need) return GM_ERR_WORKSPACE;
+  if (gm_status st = check_device()) return st;
+  return from_hip(gm::launch_tensor_list(p, g, m, v, p16, g_bf16, numel, n, list, stream));
+}
+
+GM_EXPORT gm_status gm_grad_norm(const void* list, size_t list_bytes, float max_norm, float* norm, float* coef, void* ws,
+                                 size_t ws_bytes, gm_stream_t stream) {
+  if (!list || !norm || !coef) return GM_ERR_NULL;
+  if (!(max_norm > 0.0f)) return GM_ERR_VALUE;
+  if (!aligned16(list) || !aligned4(norm) || !aligned4(coef)) return GM_ERR_ALIGN;
+  if (list_bytes < gm::list_bytes_of(1, 0)) return GM_ERR_WORKSPACE;
+  if (!ws || ws_bytes < GM_GRAD_NORM_WORKSPACE_BYTES) return GM_ERR_WORKSPACE;
+  if (!aligned16(ws)) return GM_ERR_ALIGN;
+  static_assert(GM_GRAD_NORM_WORKSPACE_BYTES >= gm::kNormBlocks * sizeof(double), "one partial sum per block");
+  if (gm_status st = check_device()) return st;
+  return from_hip(gm::launch_grad_norm(list, list_bytes, max_norm, norm, coef, static_cast<double*>(ws), stream));
+}
+
+GM_EXPORT gm_status gm_adamw_list(const void* list, size_t list_bytes, double lr, double beta1, double beta2,
+                                  double eps, double weight_decay, int32_t step, const float* coef,
+                                  gm_stream_t stream) {
+  if (!list) return GM_ERR_NULL;
+  if (gm_status st = check_adamw(lr, beta1, beta2, eps, weight_decay, step)) return st;
+  if (!aligned16(list) || (coef && !aligned4(coef))) return GM_ERR_ALIGN;
+  if (list_bytes < gm::list_bytes_of(1, 0)) return GM_ERR_WORKSPACE;
+  if (gm_status st = check_device()) return st;
+  return from_hip(gm::launch_adamw_list(list, list_bytes, lr, beta1, beta2, eps, weight_decay, step, coef, stream));
 }

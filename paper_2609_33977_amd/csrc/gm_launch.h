@@ -6,6 +6,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "gm_lora.h"
 #include "gm_plan.h"
 
 namespace gm {
@@ -86,5 +87,33 @@ hipError_t launch_hyper_bwd(const float* dlogits, const float* z, const float* g
                             const HyperWs& w, hipStream_t s);
 hipError_t launch_adamw(float* p, const float* g, float* m, float* v, int64_t n, double lr, double beta1,
                         double beta2, double eps, double weight_decay, int step, hipStream_t s);
+
+// Low-rank adapters beside a masked or packed linear.
+struct LoraShape {
+  int T, n, d_in, d_out, parts, r;  // d_out: all parts
+  int widths[kLoraMaxParts];
+};
+struct LoraBwdWs {
+  float* part;   // [splits][T][parts r] partial sums of Q
+  float* Q;      // [T][parts r], rows in the plan's order
+  float* partA;  // [gradient tiles][parts r][d_in]
+  float* partB;  // [gradient tiles][d_out][r]
+};
+hipError_t launch_lora_plan(const int* adapter, int T, int n, void* plan, hipStream_t s);
+hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, const float* scale,
+                           const void* plan, const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* Y,
+                           int64_t ldy, float* P, float* part, int splits, hipStream_t s);
+hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64_t ldx, const uint16_t* A,
+                           const uint16_t* B, const float* scale, const void* plan, const float* P,
+                           const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* dX, int64_t lddx,
+                           float* dA, float* dB, const LoraBwdWs& w, int splits, hipStream_t s);
+
+// Lists of tensors: the global gradient norm and AdamW over them.
+hipError_t launch_tensor_list(float* const* p, const void* const* g, float* const* m, float* const* v,
+                              uint16_t* const* p16, const uint8_t* g_bf16, const int64_t* numel, int n, void* list, hipStream_t s);
+hipError_t launch_grad_norm(const void* list, size_t list_bytes, float max_norm, float* norm, float* coef,
+                            double* part, hipStream_t s);
+hipError_t launch_adamw_list(const void* list, size_t list_bytes, double lr, double beta1, double beta2, double eps,
+                             double weight_decay, int step, const float* coef, hipStream_t s);
 
 }  // namespace gm

@@ -1,0 +1,62 @@
+// Sizes and layouts that the host layer and the kernels of the low-rank
+// adapters share (host arithmetic only).
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace gm {
+
+constexpr int kLoraTile = 64;       // tokens of one adapter that a block of the products works on
+constexpr int kLoraMaxParts = 4;    // projections stacked side by side
+constexpr int kLoraSlice = 512;     // contraction length that a block takes at a time: 128 per wave
+constexpr int kLoraGradCols = 128;  // columns of a gradient tile
+constexpr int32_t kLoraMagic = 0x61d7a3c5;
+
+// Tokens of one adapter whose gradient products one block sums up: longer runs
+// cost fewer partial sums, shorter ones fill the chip.
+inline int lora_grad_tokens(int64_t T) { return T > 4096 ? 512 : 256; }
+
+// Most tiles of `tile` tokens that T tokens in m buckets can need.
+inline int64_t lora_tiles(int64_t T, int64_t buckets, int64_t tile) {
+  const int64_t m = buckets < T ? buckets : T;
+  return (T + (tile - 1) * m) / tile;
+}
+
+// The plan, in 4-byte words: a header (magic, T, n, tiles, gradient tiles),
+// the tokens in the order of their adapters (those without one last), where each adapter's
+// tokens and gradient tiles start, and both tile tables (position, tokens, adapter, only tile of its adapter).
+struct LoraPlanLayout {
+  size_t order, start, gstart, tiles, gtiles, words;
+  int64_t max_tiles, max_gtiles;
+};
+
+inline LoraPlanLayout lora_plan_layout(int64_t T, int64_t n) {
+  LoraPlanLayout L;
+  L.max_tiles = lora_tiles(T, n + 1, kLoraTile);
+  L.max_gtiles = lora_tiles(T, n, lora_grad_tokens(T));
+  size_t at = 16;
+  auto take = [&](size_t& w, size_t words) {
+    w = at;
+    at = (at + words + 15) / 16 * 16;
+  };
+  take(L.order, size_t(T));
+  take(L.start, size_t(n) + 2);
+  take(L.gstart, size_t(n) + 1);
+  take(L.tiles, size_t(L.max_tiles) * 4);
+  take(L.gtiles, size_t(L.max_gtiles) * 4);
+  L.words = at;
+  return L;
+}
+
+// Blocks that share a tile's contraction over K: enough to fill the chip with
+// `tiles` tiles, at least one slice each, and few enough that their partial
+// sums stay small beside the operand.
+inline int lora_splits(int64_t tiles, int64_t K) {
+  const int64_t slices = (K + kLoraSlice - 1) / kLoraSlice;
+  int64_t ks = 512 / (tiles < 512 ? tiles : 512);
+  if (ks < 2) ks = 2;
+  return int(ks < slices ? ks : slices);
+}
+
+}  // namespace gm

@@ -21,10 +21,9 @@
 //   gru_wgrad_kernel   weight and bias gradients from the per-step gate gradients
 //   adamw_kernel       AdamW over a flat parameter vector (the GRU's)
 // Every reduction runs in a fixed order, so results are deterministic.
+#include "gm_adamw.h"
 #include "gm_device.h"
 #include "gm_launch.h"
-
-#include <math.h>
 
 namespace gm {
 
@@ -249,18 +248,6 @@ __global__ __launch_bounds__(256) void head_fwd_kernel(const float* __restrict__
   }
 }
 
-// One AdamW step on a float4 of parameters (decoupled decay, bias-corrected moments).
-// The coefficients are formed in fp64 on the host and rounded once (1 - beta
-// directly, not from a rounded beta).
-struct AdamW {
-  float lr, b1, omb1, b2, omb2, eps, decay, bc1, bc2;  // decay = 1 - lr weight_decay; bc = 1 / (1 - beta^t)
-  __device__ __forceinline__ float step(float p, float g, float& m, float& v) const {
-    m = b1 * m + omb1 * g;
-    v = b2 * v + omb2 * g * g;
-    return p * decay - lr * (m * bc1) / (sqrtf(v * bc2) + eps);
-  }
-};
-
 template <int H>
 __global__ __launch_bounds__(256) void head_bwd_kernel(const float* __restrict__ dl, float* __restrict__ A,
                                                        float* __restrict__ cb, float* __restrict__ mA,
@@ -458,20 +445,6 @@ __global__ __launch_bounds__(256) void adamw_kernel(float* __restrict__ p, const
 // ---------------------------------------------------------------- launchers
 
 int hyper_max_chunks(int64_t G_total, int L) { return int((G_total + kHeadRows - 1) / kHeadRows) + L; }
-
-static AdamW make_adamw(double lr, double b1, double b2, double eps, double wd, int step) {
-  AdamW o;
-  o.lr = float(lr);
-  o.b1 = float(b1);
-  o.omb1 = float(1.0 - b1);
-  o.b2 = float(b2);
-  o.omb2 = float(1.0 - b2);
-  o.eps = float(eps);
-  o.decay = float(1.0 - lr * wd);
-  o.bc1 = float(1.0 / (1.0 - pow(b1, double(step))));
-  o.bc2 = float(1.0 / (1.0 - pow(b2, double(step))));
-  return o;
-}
 
 // One block per direction, kUnitLanes lanes per hidden unit.
 #define GM_HYPER_CASE(KERNEL, HV, ...) \
