@@ -317,7 +317,7 @@ int lora_bwd_splits(const gm::LoraShape& z) {
 
 // Workspace of the adapters' backward, each part 256-byte aligned (see gm::LoraBwdWs).
 struct LoraBwdLayout {
-  size_t part, Q, partA, partB, total;
+  size_t part, Qn, Qt, Pt, partA, partB, total;
 };
 
 LoraBwdLayout lora_bwd_layout(const gm::LoraShape& z) {
@@ -330,7 +330,11 @@ LoraBwdLayout lora_bwd_layout(const gm::LoraShape& z) {
     off = round_up(off + bytes, 256);
   };
   take(Y.part, size_t(lora_bwd_splits(z)) * low);
-  take(Y.Q, low);
+  const size_t rows = size_t(gm::lora_plan_layout(z.T, z.n).max_tiles) * gm::kLoraTile;
+  const size_t bq = size_t((z.parts * z.r + 15) / 16), bp = size_t(z.parts) * size_t((z.r + 15) / 16);
+  take(Y.Qn, rows * bq * 32 * sizeof(uint16_t));
+  take(Y.Qt, rows * bq * 48 * sizeof(uint16_t));
+  take(Y.Pt, rows * bp * 48 * sizeof(uint16_t));
   take(Y.partA, g * z.parts * z.r * z.d_in * sizeof(float));
   take(Y.partB, g * z.d_out * z.r * sizeof(float));
   Y.total = off;
@@ -741,7 +745,8 @@ GM_EXPORT gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t
   if (gm_status st = check_device()) return st;
   char* b = static_cast<char*>(ws);
   auto f = [&](size_t off) { return reinterpret_cast<float*>(b + off); };
-  const gm::LoraBwdWs w = {f(Y.part), f(Y.Q), f(Y.partA), f(Y.partB)};
+  auto h = [&](size_t off) { return reinterpret_cast<uint16_t*>(b + off); };
+  const gm::LoraBwdWs w = {f(Y.part), h(Y.Qn), h(Y.Qt), h(Y.Pt), f(Y.partA), f(Y.partB)};
   return from_hip(gm::launch_lora_bwd(dY, lddy, X, ldx, A, B, scale, plan, P, z, base, ld_base, dX, lddx, dA, dB, w,
                                       lora_bwd_splits(z), stream));
 }

@@ -95,7 +95,9 @@ struct LoraShape {
 };
 struct LoraBwdWs {
   float* part;   // [splits][T][parts r] partial sums of Q
-  float* Q;      // [T][parts r], rows in the plan's order
+  uint16_t* Qn;  // [tiles][64][blocks][2][16]: two bf16 terms of Q, blocks of 16 ranks
+  uint16_t* Qt;  // [tiles][2][blocks][3][64][8]: three terms, tokens contracted
+  uint16_t* Pt;  // the same of P, part by part
   float* partA;  // [gradient tiles][parts r][d_in]
   float* partB;  // [gradient tiles][d_out][r]
 };

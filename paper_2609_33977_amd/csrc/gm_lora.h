@@ -23,11 +23,13 @@ inline int64_t lora_tiles(int64_t T, int64_t buckets, int64_t tile) {
   return (T + (tile - 1) * m) / tile;
 }
 
-// The plan, in 4-byte words: a header (magic, T, n, tiles, gradient tiles),
-// the tokens in the order of their adapters (those without one last), where each adapter's
-// tokens and gradient tiles start, and both tile tables (position, tokens, adapter, only tile of its adapter).
+// The plan, in 4-byte words: a header (magic, T, n, tiles, gradient tiles);
+// the tile table, tokens of one adapter at a time, those without one last
+// (first position in that order, tokens, adapter, 0); 64 tokens for every tile
+// (the last one repeated); the gradient tile table (first tile, tokens,
+// adapter, only tile of its adapter); and each adapter's first gradient tile.
 struct LoraPlanLayout {
-  size_t order, start, gstart, tiles, gtiles, words;
+  size_t tiles, tokens, gtiles, gstart, words;
   int64_t max_tiles, max_gtiles;
 };
 
@@ -40,11 +42,10 @@ inline LoraPlanLayout lora_plan_layout(int64_t T, int64_t n) {
     w = at;
     at = (at + words + 15) / 16 * 16;
   };
-  take(L.order, size_t(T));
-  take(L.start, size_t(n) + 2);
-  take(L.gstart, size_t(n) + 1);
   take(L.tiles, size_t(L.max_tiles) * 4);
+  take(L.tokens, size_t(L.max_tiles) * kLoraTile);
   take(L.gtiles, size_t(L.max_gtiles) * 4);
+  take(L.gstart, size_t(n) + 1);
   L.words = at;
   return L;
 }

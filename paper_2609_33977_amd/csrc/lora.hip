@@ -18,11 +18,11 @@
 #include "gm_device.h"
 #include "gm_launch.h"
 #include "gm_lora.h"
+#include "gm_pipe.h"
 
 namespace gm {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef short lora_i16x4 __attribute__((ext_vector_type(4)));
 
 // C [16 x 16] += A [16 x 32] B [32 x 16]: lane l supplies A row (l % 16) and B
 // column (l % 16), each over k = 8 (l / 16) .. + 7, and holds C rows
@@ -39,25 +39,28 @@ struct LoraTile {
 };
 
 struct LoraPlan {
-  const int* order;
-  const int* start;
-  const int* gstart;
-  const LoraTile* tiles;
-  const LoraTile* gtiles;
   const int* head;
+  const LoraTile* tiles;
+  const int* tokens;
+  const LoraTile* gtiles;
+  const int* gstart;
   int T, n;
-  // A plan made for other sizes is not followed: no tile of it is valid.
-  __device__ __forceinline__ bool valid() const { return head[0] == kLoraMagic && head[1] == T && head[2] == n; }
+  // Tile i of the table, without tokens if there is none: past the last, or in a
+  // plan that was made for other sizes.  Header, entry and the tile's tokens do not wait for one another.
+  __device__ __forceinline__ LoraTile tile(const LoraTile* table, int i, int which) const {
+    const int magic = head[0], hT = head[1], hn = head[2], count = head[which];
+    LoraTile t = table[i];
+    if (magic != kLoraMagic || hT != T || hn != n || i >= count) t.count = 0;
+    return t;
+  }
 };
 
 static LoraPlan lora_plan(const void* plan, int T, int n) {
   const LoraPlanLayout L = lora_plan_layout(T, n);
   const int* w = static_cast<const int*>(plan);
-  return {w + L.order, w + L.start, w + L.gstart, reinterpret_cast<const LoraTile*>(w + L.tiles),
-          reinterpret_cast<const LoraTile*>(w + L.gtiles), w, T, n};
+  return {w, reinterpret_cast<const LoraTile*>(w + L.tiles), w + L.tokens,
+          reinterpret_cast<const LoraTile*>(w + L.gtiles), w + L.gstart, T, n};
 }
-
-constexpr int kPlanWaves = 8;
 
 // Lanes of the wave with the same key, as a mask.
 __device__ __forceinline__ uint64_t same_key(int key, int bits, bool on) {
@@ -69,98 +72,119 @@ __device__ __forceinline__ uint64_t same_key(int key, int bits, bool on) {
   return m;
 }
 
+constexpr int kPlanMaxWaves = 16, kPlanBatch = 8;
+
 // A stable counting sort of the tokens by adapter in one block: each wave
 // counts and later places a contiguous run of tokens, so that equal adapters
 // keep their tokens' order and sums over them do not depend on timing.  No
 // atomics: the lanes of one key elect a leader.  One launch per batch serves
-// every linear of the model.
-__global__ __launch_bounds__(64 * kPlanWaves) void lora_plan_kernel(const int* __restrict__ adapter, int T, int n,
-                                                                    int gtokens, int* __restrict__ head,
-                                                                    int* __restrict__ order, int* __restrict__ start,
-                                                                    int* __restrict__ gstart,
-                                                                    LoraTile* __restrict__ tiles,
-                                                                    LoraTile* __restrict__ gtiles) {
-  extern __shared__ int s_count[];  // [kPlanWaves][n + 1], then the buckets' totals, first tiles and first gradient tiles
-  __shared__ int s_sum[3][64 * kPlanWaves];
-  const int nb = n + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, NT = 64 * kPlanWaves;
-  int* s_tile = s_count + kPlanWaves * nb;
+// every linear of the model.  Bound by latency: the ids of 512 tokens are loaded at a time.
+__global__ __launch_bounds__(64 * kPlanMaxWaves) void lora_plan_kernel(const int* __restrict__ adapter, int T, int n,
+                                                                       int gtokens, int* __restrict__ head,
+                                                                       LoraTile* __restrict__ tiles,
+                                                                       int* __restrict__ tokens,
+                                                                       LoraTile* __restrict__ gtiles,
+                                                                       int* __restrict__ gstart) {
+  extern __shared__ int s_count[];  // [waves][n + 1], then the buckets' first positions, tiles and gradient tiles [n + 2]
+  __shared__ int s_sum[3][kPlanMaxWaves];
+  const int nb = n + 1, tid = threadIdx.x, NT = blockDim.x, waves = NT >> 6, lane = tid & 63, wave = tid >> 6;
+  int* s_start = s_count + waves * nb;
+  int* s_tile = s_start + nb + 1;
   int* s_gtile = s_tile + nb + 1;
-  int* s_start = s_gtile + nb + 1;
-  for (int i = tid; i < kPlanWaves * nb; i += NT) s_count[i] = 0;
+  for (int i = tid; i < waves * nb; i += NT) s_count[i] = 0;
   __syncthreads();
   const int bits = 32 - __builtin_clz(n);
   const int per = (T + NT - 1) / NT * 64;  // tokens per wave
   const int t0 = min(wave * per, T), t1 = min(t0 + per, T);
   int* mine = s_count + wave * nb;
-  auto key_of = [&](int t) {
-    const int a = t < t1 ? adapter[t] : n;
-    return unsigned(a) < unsigned(n) ? a : n;
+  int ids[kPlanBatch];
+  auto load_ids = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kPlanBatch; ++i) {
+      const int a = t + 64 * i + lane < t1 ? adapter[t + 64 * i + lane] : n;
+      ids[i] = unsigned(a) < unsigned(n) ? a : n;
+    }
   };
-  for (int t = t0; t < t1; t += 64) {
-    const bool on = t + lane < t1;
-    const int key = key_of(t + lane);
-    const uint64_t m = same_key(key, bits, on);
-    if (on && (m & ((uint64_t(1) << lane) - 1)) == 0) mine[key] += __popcll(m);
-    __builtin_amdgcn_wave_barrier();
+  for (int t = t0; t < t1; t += 64 * kPlanBatch) {
+    load_ids(t);
+#pragma unroll
+    for (int i = 0; i < kPlanBatch; ++i) {
+      if (t + 64 * i >= t1) break;  // uniform
+      const bool on = t + 64 * i + lane < t1;
+      const uint64_t m = same_key(ids[i], bits, on);
+      if (on && (m & ((uint64_t(1) << lane) - 1)) == 0) mine[ids[i]] += __popcll(m);
+      __builtin_amdgcn_wave_barrier();
+    }
   }
   __syncthreads();
   // Totals of a run of buckets per thread, scanned over the block; a wave's
   // counts become its first position within the bucket.
   const int run = (nb + NT - 1) / NT, b0 = min(tid * run, nb), b1 = min(b0 + run, nb);
-  int c = 0, ct = 0, cg = 0;
+  int c[3] = {0, 0, 0};
   for (int b = b0; b < b1; ++b) {
     int tot = 0;
-    for (int w = 0; w < kPlanWaves; ++w) {
+    for (int w = 0; w < waves; ++w) {
       const int k = s_count[w * nb + b];
       s_count[w * nb + b] = tot;
       tot += k;
     }
-    s_start[b] = c, s_tile[b] = ct, s_gtile[b] = cg;
-    c += tot;
-    ct += (tot + kLoraTile - 1) / kLoraTile;
-    if (b < n) cg += (tot + gtokens - 1) / gtokens;
+    s_start[b] = c[0], s_tile[b] = c[1], s_gtile[b] = c[2];
+    c[0] += tot;
+    c[1] += (tot + kLoraTile - 1) / kLoraTile;
+    if (b < n) c[2] += (tot + gtokens - 1) / gtokens;
   }
-  s_sum[0][tid] = c, s_sum[1][tid] = ct, s_sum[2][tid] = cg;
+  int e[3];
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    e[q] = c[q];
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(e[q], d);
+      if (lane >= d) e[q] += up;
+    }
+    if (lane == 63) s_sum[q][wave] = e[q];
+  }
   __syncthreads();
-  for (int d = 1; d < NT; d <<= 1) {
-    int add[3] = {0, 0, 0};
-    if (tid >= d)
-      for (int q = 0; q < 3; ++q) add[q] = s_sum[q][tid - d];
-    __syncthreads();
-    for (int q = 0; q < 3; ++q) s_sum[q][tid] += add[q];
-    __syncthreads();
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    e[q] -= c[q];
+    for (int w = 0; w < wave; ++w) e[q] += s_sum[q][w];
   }
-  const int e = s_sum[0][tid] - c, et = s_sum[1][tid] - ct, eg = s_sum[2][tid] - cg;
-  for (int b = b0; b < b1; ++b) s_start[b] += e, s_tile[b] += et, s_gtile[b] += eg;
+  for (int b = b0; b < b1; ++b) s_start[b] += e[0], s_tile[b] += e[1], s_gtile[b] += e[2];
   if (tid == NT - 1) {
     s_start[nb] = T;
-    s_tile[nb] = s_sum[1][tid];
-    s_gtile[nb] = s_sum[2][tid];
-    head[0] = kLoraMagic, head[1] = T, head[2] = n, head[3] = s_sum[1][tid], head[4] = s_sum[2][tid];
+    s_tile[nb] = e[1] + c[1];
+    s_gtile[nb] = e[2] + c[2];
+    head[0] = kLoraMagic, head[1] = T, head[2] = n, head[3] = e[1] + c[1], head[4] = e[2] + c[2];
   }
   __syncthreads();
-  for (int b = tid; b <= nb; b += NT) {
-    start[b] = s_start[b];
-    if (b <= n) gstart[b] = s_gtile[b];
+  for (int b = tid; b <= n; b += NT) gstart[b] = s_gtile[b];
+  for (int t = t0; t < t1; t += 64 * kPlanBatch) {
+    if (per > 64 * kPlanBatch) load_ids(t);  // else they are still there
+#pragma unroll
+    for (int i = 0; i < kPlanBatch; ++i) {
+      if (t + 64 * i >= t1) break;  // uniform
+      const bool on = t + 64 * i + lane < t1;
+      const int key = ids[i];
+      const uint64_t m = same_key(key, bits, on);
+      const uint64_t before = m & ((uint64_t(1) << lane) - 1);
+      const int at = on ? mine[key] : 0;
+      __builtin_amdgcn_wave_barrier();
+      if (on) tokens[s_tile[key] * kLoraTile + at + __popcll(before)] = t + 64 * i + lane;
+      if (on && before == 0) mine[key] += __popcll(m);
+      __builtin_amdgcn_wave_barrier();
+    }
   }
-  for (int b = wave; b < nb; b += kPlanWaves) {
+  __syncthreads();
+  for (int b = wave; b < nb; b += waves) {
     const int p = s_start[b], tot = s_start[b + 1] - p;
     const int nt = s_tile[b + 1] - s_tile[b], ng = s_gtile[b + 1] - s_gtile[b];
+    if (tot == 0) continue;
     for (int i = lane; i < nt; i += 64)
-      tiles[s_tile[b] + i] = {p + i * kLoraTile, min(kLoraTile, tot - i * kLoraTile), b, nt == 1};
+      tiles[s_tile[b] + i] = {p + i * kLoraTile, min(kLoraTile, tot - i * kLoraTile), b, 0};
     for (int i = lane; i < ng; i += 64)
-      gtiles[s_gtile[b] + i] = {p + i * gtokens, min(gtokens, tot - i * gtokens), b, ng == 1};
-  }
-  for (int t = t0; t < t1; t += 64) {
-    const bool on = t + lane < t1;
-    const int key = key_of(t + lane);
-    const uint64_t m = same_key(key, bits, on);
-    const uint64_t before = m & ((uint64_t(1) << lane) - 1);
-    const int at = on ? s_start[key] + mine[key] : 0;
-    __builtin_amdgcn_wave_barrier();
-    if (on) order[at + __popcll(before)] = t + lane;
-    if (on && before == 0) mine[key] += __popcll(m);
-    __builtin_amdgcn_wave_barrier();
+      gtiles[s_gtile[b] + i] = {s_tile[b] + i * (gtokens / kLoraTile), min(gtokens, tot - i * gtokens), b, ng == 1};
+    int* slots = tokens + s_tile[b] * kLoraTile;
+    if (tot + lane < nt * kLoraTile) slots[tot + lane] = slots[tot - 1];
   }
 }
 
@@ -172,101 +196,132 @@ struct LoraDown {
   const uint16_t* W;  // one adapter's weights: [wrows, K] (A) or [K, wrows] (B, one part)
   int64_t wstride;    // elements from one adapter to the next
   int K, wrows;
-  float* part;  // [splits][T][R]
+  float* part;  // [splits][T][R], rows in the plan's order
   int R;
   int splits, slice;  // K per split, a multiple of kLoraSlice
   int off[kLoraMaxParts], width[kLoraMaxParts];  // B: the parts' columns
   int chunks;                                    // blocks of 16 RT ranks per part
 };
 
-// part[s][p][c] = sum over split s's K range of X[order[p]][k] W[c][k].  A
+// part[s][p][c] = sum over split s's K range of X[token p][k] W[c][k].  A
 // block takes a tile of up to 64 tokens; its waves take 128 of every 512 k, so
 // that an adapter's fragment is loaded once and used for all four 16-token
-// fragments, and add up through LDS.  All fragments of a wave's 128 k are loaded before
-// they are used: 16 KiB in flight per wave.  B is contracted over its rows: 128 of them go
-// through LDS and come back transposed.
+// fragments, and add up through LDS.  Fragments come straight from memory into
+// registers, four steps of 32 k ahead of their use.  B is contracted over its
+// rows: 128 of them go through LDS and come back transposed.
 template <int RT, bool BMAJOR, int NSUB>
-__device__ __forceinline__ void lora_down_body(const LoraDown& a, const LoraTile& tile, const LoraPlan& plan, int split,
-                                               int chunk, int part, float* s_red, u32x4* s_w) {
+__device__ __forceinline__ void lora_down_body(const LoraDown& a, const LoraTile& tile, const LoraPlan& plan,
+                                               const int (&tok)[4], int split, int chunk, int part, float* s_red,
+                                               u32x4* s_w) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const int r0 = chunk * 16 * RT, nr = min(16 * RT, a.wrows - r0);
   const int col0 = BMAJOR ? a.off[part] : 0, K = BMAJOR ? a.width[part] : a.K;
   const int k0 = split * a.slice, k1 = min(k0 + a.slice, K);
   const uint16_t* xr[NSUB];
 #pragma unroll
-  for (int s = 0; s < NSUB; ++s)
-    xr[s] = a.X + int64_t(plan.order[tile.pos + min(s * 16 + row, tile.count - 1)]) * a.ldx + col0;
+  for (int s = 0; s < NSUB; ++s) xr[s] = a.X + int64_t(tok[s]) * a.ldx + col0;
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride;
-  if (BMAJOR) w += int64_t(col0) * a.wrows;
   f32x4 acc[NSUB][RT];
 #pragma unroll
   for (int s = 0; s < NSUB; ++s)
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[s][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int kb = k0; kb < k1; kb += kLoraSlice) {
-    const int kw = kb + wave * 128;
-    u32x4 x[NSUB][4], wf[RT][4];
+  u32x4 x[NSUB][4];
+  // Past the range's end a row's last values stand in, against zeros of the adapter.
+  auto load_x = [&](int kw, int j) {
+    const int k = min(kw + 32 * j + 8 * q, k1 - 8);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = kw + 32 * j + 8 * q;
-      const bool in = k < k1;
+    for (int s = 0; s < NSUB; ++s) x[s][j] = ld16(xr[s] + k);
+  };
+  if (k0 < k1) {
+    if constexpr (!BMAJOR) {
+      u32x4 wf[RT][4];
+      const uint16_t* wr[RT];
 #pragma unroll
-      for (int s = 0; s < NSUB; ++s) x[s][j] = in ? ld16(xr[s] + k) : zero16();
-      if constexpr (!BMAJOR) {
+      for (int t = 0; t < RT; ++t) wr[t] = w + int64_t(r0 + min(t * 16 + row, nr - 1)) * K;
+      auto load_w = [&](int kw, int j) {
+        const int k = kw + 32 * j + 8 * q;
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-          wf[t][j] = in ? ld16(w + int64_t(r0 + min(t * 16 + row, nr - 1)) * K + k) : zero16();
+        for (int t = 0; t < RT; ++t) wf[t][j] = ld16(wr[t] + min(k, k1 - 8));
+      };
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
+      for (int kb = k0; kb < k1; kb += kLoraSlice) {
+        const int kw = kb + wave * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool in = kw + 32 * j + 8 * q < k1;
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            const u32x4 f = in ? wf[t][j] : zero16();
+#pragma unroll
+            for (int s = 0; s < NSUB; ++s) acc[s][t] = mfma16(x[s][j], f, acc[s][t]);
+          }
+          if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
+        }
       }
-    }
-    if constexpr (BMAJOR) {
+    } else {
       constexpr int CH = 2 * RT;  // 16-byte chunks per row of 16 RT ranks
+      w += int64_t(col0) * a.wrows + r0;
       u32x4* sw = s_w + wave * 128 * CH;
       u32x4 v[CH * 2];
+      auto load_w = [&](int kw) {
 #pragma unroll
-      for (int i = 0; i < CH * 2; ++i) {
-        const int e = i * 64 + lane, k = kw + e / CH, c = 8 * (e % CH);
-        v[i] = k < k1 && c < nr ? ld16(w + int64_t(k) * a.wrows + r0 + c) : zero16();
-      }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int i = 0; i < CH * 2; ++i) sw[i * 64 + lane] = v[i];
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      // the 16-lane group q reads rows 8 q + (row / 4) and + 4 of each 32, columns 4 (row % 4) .. + 3
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          const char* b = reinterpret_cast<const char*>(sw) + (32 * j + 8 * q + (row >> 2)) * (CH * 16) + t * 32 + 8 * (row & 3);
-          const lora_i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) lora_i16x4*)b);
-          const lora_i16x4 hi =
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) lora_i16x4*)(b + 4 * CH * 16));
-          __builtin_memcpy(&wf[t][j], &lo, 8);
-          __builtin_memcpy(reinterpret_cast<char*>(&wf[t][j]) + 8, &hi, 8);
+        for (int i = 0; i < CH * 2; ++i) {
+          const int e = i * 64 + lane, k = min(kw + e / CH, k1 - 1), c = min(8 * (e % CH), nr - 8);
+          v[i] = ld16(w + int64_t(k) * a.wrows + c);
         }
+      };
+      load_w(k0 + wave * 128);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j);
+      for (int kb = k0; kb < k1; kb += kLoraSlice) {
+        const int kw = kb + wave * 128;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < CH * 2; ++i) {
+          const int k = kw + (i * 64 + lane) / CH;
+          sw[i * 64 + lane] = k < k1 ? v[i] : zero16();
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (kb + kLoraSlice < k1) load_w(kw + kLoraSlice);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            // the 16-lane group q reads rows 8 q + (row / 4) and + 4 of the 32, columns 4 (row % 4) .. + 3
+            const char* b =
+                reinterpret_cast<const char*>(sw) + (32 * j + 8 * q + (row >> 2)) * (CH * 16) + t * 32 + 8 * (row & 3);
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)b);
+            const i16x4 hi =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(b + 4 * CH * 16));
+            u32x4 f;
+            __builtin_memcpy(&f, &lo, 8);
+            __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+#pragma unroll
+            for (int s = 0; s < NSUB; ++s) acc[s][t] = mfma16(x[s][j], f, acc[s][t]);
+          }
+          if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j);
+        }
+      }
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int s = 0; s < NSUB; ++s)
-#pragma unroll
-        for (int t = 0; t < RT; ++t) acc[s][t] = mfma16(x[s][j], wf[t][j], acc[s][t]);
   }
   float* out = a.part + (int64_t(split) * plan.T + tile.pos) * a.R + part * a.wrows + r0;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     if (t * 16 >= nr) break;  // uniform
-    __syncthreads();
+    if (t > 0) __syncthreads();
 #pragma unroll
     for (int s = 0; s < NSUB; ++s)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s_red[(wave * 64 + s * 16 + 4 * q + i) * 17 + row] = acc[s][t][i];
     __syncthreads();
     for (int e = threadIdx.x; e < NSUB * 256; e += 256) {
-      const int tok = e >> 4, c = e & 15;
-      const float v = (s_red[tok * 17 + c] + s_red[(64 + tok) * 17 + c]) +
-                      (s_red[(128 + tok) * 17 + c] + s_red[(192 + tok) * 17 + c]);
-      if (tok < tile.count && t * 16 + c < nr) out[int64_t(tok) * a.R + t * 16 + c] = v;
+      const int i = e >> 4, c = e & 15;
+      const float v =
+          (s_red[i * 17 + c] + s_red[(64 + i) * 17 + c]) + (s_red[(128 + i) * 17 + c] + s_red[(192 + i) * 17 + c]);
+      if (i < tile.count && t * 16 + c < nr) out[int64_t(i) * a.R + t * 16 + c] = v;
     }
   }
 }
@@ -275,60 +330,127 @@ template <int RT, bool BMAJOR>
 __global__ __launch_bounds__(256) void lora_down_kernel(LoraDown a, LoraPlan plan) {
   __shared__ float s_red[256 * 17];
   __shared__ u32x4 s_w[BMAJOR ? 4 * 128 * 2 * RT : 1];
-  if (!plan.valid()) return;
   const int split = blockIdx.x % a.splits, ti = blockIdx.x / a.splits;
-  if (ti >= plan.head[3]) return;
-  const LoraTile tile = plan.tiles[ti];
-  if (tile.adapter >= plan.n) return;
+  int tok[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
+  const LoraTile tile = plan.tile(plan.tiles, ti, 3);
+  if (tile.count == 0 || tile.adapter >= plan.n) return;
   const int chunk = blockIdx.y % a.chunks, part = BMAJOR ? blockIdx.y / a.chunks : 0;
   if (tile.count <= 16)
-    lora_down_body<RT, BMAJOR, 1>(a, tile, plan, split, chunk, part, s_red, s_w);
+    lora_down_body<RT, BMAJOR, 1>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
   else if (tile.count <= 32)
-    lora_down_body<RT, BMAJOR, 2>(a, tile, plan, split, chunk, part, s_red, s_w);
+    lora_down_body<RT, BMAJOR, 2>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
   else
-    lora_down_body<RT, BMAJOR, 4>(a, tile, plan, split, chunk, part, s_red, s_w);
+    lora_down_body<RT, BMAJOR, 4>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
 }
 
-// Q[p][c] = scale sum_s part[s][p][c]
-__global__ __launch_bounds__(256) void lora_sum_kernel(const float* __restrict__ part, int splits, int R,
-                                                       const float* __restrict__ scale, LoraPlan plan,
-                                                       float* __restrict__ Q) {
-  if (!plan.valid()) return;
-  const int ti = blockIdx.x;
-  if (ti >= plan.head[3]) return;
-  const LoraTile tile = plan.tiles[ti];
-  if (tile.adapter >= plan.n) return;
-  const float c = scale[tile.adapter];
-  const int64_t at = int64_t(tile.pos) * R;
-  for (int e = 4 * threadIdx.x; e < tile.count * R; e += 1024) {
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) v += *reinterpret_cast<const f32x4*>(part + int64_t(s) * plan.T * R + at + e);
-    *reinterpret_cast<f32x4*>(Q + at + e) = v * c;
+// Sum of the splits' partial sums at p, four values.
+__device__ __forceinline__ f32x4 sum_splits(const float* p, int splits, int64_t stride) {
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < splits; s += 8) {
+    f32x4 u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4*>(p + min(s + i, splits - 1) * stride);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s + i < splits) v += u[i];
+  }
+  return v;
+}
+
+// ---------------------------------------------------------------- bf16 terms of fp32 values
+
+// What bf16 term `term` leaves of x.  An infinity is all in the first.
+__device__ __forceinline__ float lora_rest(float x, uint32_t term) {
+  const float h = __uint_as_float(term << 16);
+  return (term & 0x7f80u) == 0x7f80u ? 0.0f : x - h;
+}
+
+// The first N terms of eight values.
+template <int N>
+__device__ __forceinline__ void lora_terms(const float (&x)[8], u32x4 (&f)[N]) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    float a = x[2 * p], b = x[2 * p + 1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f[i][p] = pack_bf16x2(a, b);
+      a = lora_rest(a, f[i][p] & 0xffffu), b = lora_rest(b, f[i][p] >> 16);
+    }
+  }
+}
+
+struct LoraTerms {
+  const float* part;  // [splits][T][R]: Q before its scale
+  int splits, R;
+  const float* scale;
+  const float* P;  // [T, R] in the tokens' order
+  int r, parts;
+  uint16_t* Qn;  // [tile][64][blocks of 16 ranks][2 terms][16], or nullptr
+  uint16_t* Qt;  // [tile][2][blocks][3 terms][64 lanes][8]: fragments over 32 tokens
+  uint16_t* Pt;  // the same of P, the parts' blocks one after the other
+  int blocksQ, blocksP;  // blocks of 16 ranks (0: not wanted)
+};
+
+// Splits Q and P into the bf16 terms that the products below multiply with, once for all columns: of Q
+// two terms row by row for dX, and three of both in the order in which a wave's lanes hold them as a
+// fragment with the tokens contracted.  Rows past a tile's tokens and ranks past the last are zeros.
+__global__ __launch_bounds__(256) void lora_terms_kernel(LoraTerms a, LoraPlan plan) {
+  __shared__ float s_v[64 * 17];
+  const int blocks = a.blocksQ + a.blocksP, ti = blockIdx.x / blocks, b = blockIdx.x % blocks;
+  const int row = threadIdx.x >> 2, c = 4 * (threadIdx.x & 3);
+  const int token = plan.tokens[ti * kLoraTile + row];
+  const LoraTile tile = plan.tile(plan.tiles, ti, 3);
+  if (tile.count == 0 || tile.adapter >= plan.n) return;
+  const bool isq = b < a.blocksQ;
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (isq) {
+    if (row < tile.count && 16 * b + c < a.R)
+      v = sum_splits(a.part + int64_t(tile.pos + row) * a.R + 16 * b + c, a.splits, int64_t(plan.T) * a.R) *
+          a.scale[tile.adapter];
+  } else {
+    const int per = a.blocksP / a.parts, part = (b - a.blocksQ) / per, k = 16 * ((b - a.blocksQ) % per) + c;
+    if (row < tile.count && k < a.r) v = *reinterpret_cast<const f32x4*>(a.P + int64_t(token) * a.R + part * a.r + k);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s_v[row * 17 + c + i] = v[i];
+  __syncthreads();
+  if (isq && a.Qn && threadIdx.x < 128) {
+    const int r = threadIdx.x >> 1, h = threadIdx.x & 1;
+    float x[8];
+    u32x4 f[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s_v[r * 17 + 8 * h + i];
+    lora_terms<2>(x, f);
+    uint16_t* out = a.Qn + ((int64_t(ti) * kLoraTile + r) * a.blocksQ + b) * 32 + 8 * h;
+    st16(out, f[0]);
+    st16(out + 16, f[1]);
+  }
+  uint16_t* frag = isq ? a.Qt : a.Pt;
+  if (frag && threadIdx.x >= 128) {
+    const int h = (threadIdx.x >> 6) & 1, lane = threadIdx.x & 63, k = lane & 15, q = lane >> 4;
+    const int fb = isq ? b : b - a.blocksQ, fblocks = isq ? a.blocksQ : a.blocksP;
+    float x[8];
+    u32x4 f[3];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = s_v[(32 * h + 8 * q + i) * 17 + k];
+    lora_terms<3>(x, f);
+    uint16_t* out = frag + ((int64_t(ti) * 2 + h) * fblocks + fb) * (3 * 512) + lane * 8;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) st16(out + 512 * i, f[i]);
   }
 }
 
 // ---------------------------------------------------------------- products with the rank contracted
 
-// The first two bf16 terms of eight fp32 values.  An infinity is all in the first.
-__device__ __forceinline__ float lora_rest(float x, uint32_t term) {
-  const float h = __uint_as_float(term << 16);
-  return (term & 0x7f80u) == 0x7f80u ? 0.0f : x - h;
-}
-__device__ __forceinline__ void lora_terms(const float (&x)[8], u32x4& hi, u32x4& lo) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    hi[p] = pack_bf16x2(x[2 * p], x[2 * p + 1]);
-    lo[p] = pack_bf16x2(lora_rest(x[2 * p], hi[p] & 0xffffu), lora_rest(x[2 * p + 1], hi[p] >> 16));
-  }
-}
-
 struct LoraUp {
-  const float* low;  // [splits][T][R], rows in the plan's order
+  const float* part;  // [splits][T][R], rows in the plan's order
   int splits, R;
-  const float* scale;  // nullptr: already in `low`
-  const uint16_t* W;   // B [d_out, r] or A [R, d_in] of one adapter
+  const float* scale;
+  const uint16_t* W;  // one adapter's weights: B [d_out, r] or A [R, d_in]
   int64_t wstride;
-  int r;  // ranks contracted: a part's for B, all for A
+  int r;
   const uint16_t* base;
   int64_t ld_base;
   uint16_t* Y;
@@ -338,56 +460,53 @@ struct LoraUp {
   int off[kLoraMaxParts], width[kLoraMaxParts], first[kLoraMaxParts + 1];  // first block of each part
 };
 
-// A tile's rank terms in LDS: [64 tokens][RT blocks of 16 ranks, 8 spare] bf16, the first terms, then the second.
+// A row of a tile's rank terms in LDS: per 16 ranks the first terms, then the second; 8 spare values.
 template <int RT>
-constexpr int kUpPitch = 16 * RT + 8;
+constexpr int kUpPitch = 32 * RT + 8;
 
-// Stages ranks [c0, c0 + 16 RT) of rows [t0, t0 + rows) of the tile as bf16
-// terms, zeros past the tile's tokens and past `ranks`; with `keep`, the block
-// also stores them to P.
+// Stages the ranks of `rows` rows of the tile, zeros past the tile's tokens
+// and past r; with `keep`, the block also stores them to P.
 template <int RT>
-__device__ __forceinline__ void lora_stage(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int t0, int rows,
-                                           int col0, int c0, int ranks, bool keep, uint16_t* s_hi, uint16_t* s_lo) {
-  const float c = a.scale ? a.scale[tile.adapter] : 1.0f;
+__device__ __forceinline__ void lora_stage(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int ti, int rows,
+                                           int col0, bool keep, uint16_t* s_terms) {
+  const float c = a.scale[tile.adapter];
   for (int e = threadIdx.x; e < rows * 2 * RT; e += 256) {
-    const int row = e / (2 * RT), k = 8 * (e % (2 * RT)), tok = t0 + row;
+    const int row = e / (2 * RT), h = e % (2 * RT), k = 8 * h;
     float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (tok < tile.count && c0 + k < ranks) {
-      const float* src = a.low + int64_t(tile.pos + tok) * a.R + col0 + c0 + k;
-      for (int s = 0; s < a.splits; ++s) {
-        const f32x4 u0 = *reinterpret_cast<const f32x4*>(src + int64_t(s) * plan.T * a.R);
-        const f32x4 u1 = *reinterpret_cast<const f32x4*>(src + int64_t(s) * plan.T * a.R + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += u0[i], v[4 + i] += u1[i];
-      }
+    if (row < tile.count && k < a.r) {
+      const float* src = a.part + int64_t(tile.pos + row) * a.R + col0 + k;
+      const int64_t stride = int64_t(plan.T) * a.R;
+      const f32x4 lo = sum_splits(src, a.splits, stride), hi = sum_splits(src + 4, a.splits, stride);
       if (keep) {
-        float* p = a.P + int64_t(plan.order[tile.pos + tok]) * a.R + col0 + c0 + k;
-        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        float* p = a.P + int64_t(plan.tokens[ti * kLoraTile + row]) * a.R + col0 + k;
+        *reinterpret_cast<f32x4*>(p) = lo;
+        *reinterpret_cast<f32x4*>(p + 4) = hi;
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= c;
+      for (int i = 0; i < 4; ++i) v[i] = lo[i] * c, v[4 + i] = hi[i] * c;
     }
-    u32x4 hi, lo;
-    lora_terms(v, hi, lo);
-    st16(s_hi + row * kUpPitch<RT> + k, hi);
-    st16(s_lo + row * kUpPitch<RT> + k, lo);
+    u32x4 f[2];
+    lora_terms<2>(v, f);
+    uint16_t* out = s_terms + row * kUpPitch<RT> + (h >> 1) * 32 + 8 * (h & 1);
+    st16(out, f[0]);
+    st16(out + 16, f[1]);
   }
 }
 
 // A tile of tokens without an adapter: columns of base, and zeros in P.
-__device__ __forceinline__ void lora_copy(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int col0,
+__device__ __forceinline__ void lora_copy(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int ti, int col0,
                                           int cols, int rank0, int ranks) {
+  const int* tokens = plan.tokens + ti * kLoraTile;
   if (a.base != a.Y) {
     const int cpr = cols / 8;
     for (int e = threadIdx.x; e < tile.count * cpr; e += 256) {
-      const int64_t t = plan.order[tile.pos + e / cpr];
+      const int64_t t = tokens[e / cpr];
       const int c = col0 + 8 * (e % cpr);
       st16(a.Y + t * a.ldy + c, ld16(a.base + t * a.ld_base + c));
     }
   }
   for (int e = threadIdx.x; e < tile.count * ranks; e += 256)
-    a.P[int64_t(plan.order[tile.pos + e / ranks]) * a.R + rank0 + e % ranks] = 0.0f;
+    a.P[int64_t(tokens[e / ranks]) * a.R + rank0 + e % ranks] = 0.0f;
 }
 
 __device__ __forceinline__ u32x4 lora_add8(const u32x4& b, const float (&d)[8]) {
@@ -401,145 +520,171 @@ __device__ __forceinline__ u32x4 lora_add8(const u32x4& b, const float (&d)[8]) 
 // columns tokens, with B's rows dealt so that two instructions leave eight
 // consecutive columns of one token in each lane: base and Y move as 16-byte
 // vectors straight between memory and registers, 64 bytes per token.  One
-// instruction's 32 k hold the two terms of 16 ranks.
-template <int RT, int NSUB>
-__device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int part,
-                                             int cb, const uint16_t* s_hi, const uint16_t* s_lo) {
+// instruction's 32 k hold the two terms of 16 ranks.  A wave loads UN runs of 32
+// columns at once; the first before the ranks are staged.
+template <int RT, int NSUB, int UN>
+__device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int ti,
+                                             const int (&tok)[4], int part, int cb, bool keep, uint16_t* s_terms) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
-  const int off = a.off[part], width = a.width[part];
+  const int off = a.off[part], width = a.width[part], end = min(cb + a.span, width);
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + int64_t(off) * a.r + 8 * (q & 1);
-  u32x4 pf[NSUB][RT];
-  const uint16_t* sp = (q >> 1 ? s_lo : s_hi) + row * kUpPitch<RT> + 8 * (q & 1);
   const uint16_t* br[NSUB];
   uint16_t* yr[NSUB];
 #pragma unroll
   for (int s = 0; s < NSUB; ++s) {
-#pragma unroll
-    for (int t = 0; t < RT; ++t) pf[s][t] = ld16(sp + s * 16 * kUpPitch<RT> + t * 16);
-    const int64_t tok = plan.order[tile.pos + min(s * 16 + row, tile.count - 1)];
-    yr[s] = a.Y + tok * a.ldy + off + 8 * q;
-    br[s] = a.base + tok * a.ld_base + off + 8 * q;
+    yr[s] = a.Y + int64_t(tok[s]) * a.ldy + off;
+    br[s] = a.base + int64_t(tok[s]) * a.ld_base + off;
   }
-  const int end = min(cb + a.span, width);
-  for (int o0 = cb + 32 * wave; o0 < end; o0 += 128) {
-    const bool in = o0 + 8 * q < end;
-    u32x4 wf[2][RT], b[NSUB];
+  u32x4 wf[UN][2][RT], b[UN][NSUB];
+  auto load = [&](int o0) {
 #pragma unroll
-    for (int s = 0; s < NSUB; ++s) b[s] = in ? ld16(br[s] + o0) : zero16();
+    for (int u = 0; u < UN; ++u) {
+      const int o = o0 + 128 * u;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int o = min(o0 + 8 * (row >> 2) + 4 * j + (row & 3), width - 1);
-#pragma unroll
-      for (int t = 0; t < RT; ++t)
-        wf[j][t] = t * 16 + 8 * (q & 1) < a.r ? ld16(w + int64_t(o) * a.r + t * 16) : zero16();
-    }
-#pragma unroll
-    for (int s = 0; s < NSUB; ++s) {
-      f32x4 d[2];
+      for (int s = 0; s < NSUB; ++s) b[u][s] = ld16(br[s] + min(o + 8 * q, width - 8));
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        d[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const int64_t wo = int64_t(min(o + 8 * (row >> 2) + 4 * j + (row & 3), width - 1)) * a.r;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) d[j] = mfma16(wf[j][t], pf[s][t], d[j]);
+        for (int t = 0; t < RT; ++t)
+          wf[u][j][t] = t * 16 + 8 * (q & 1) < a.r ? ld16(w + wo + t * 16) : zero16();
       }
-      const float v[8] = {d[0][0], d[0][1], d[0][2], d[0][3], d[1][0], d[1][1], d[1][2], d[1][3]};
-      if (in && s * 16 + row < tile.count) st16(yr[s] + o0, lora_add8(b[s], v));
     }
+  };
+  int o0 = cb + 32 * wave;
+  load(o0);
+  lora_stage<RT>(a, plan, tile, ti, 16 * NSUB, part * a.r, keep, s_terms);
+  __syncthreads();
+  u32x4 pf[NSUB][RT];
+#pragma unroll
+  for (int s = 0; s < NSUB; ++s)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) pf[s][t] = ld16(s_terms + (s * 16 + row) * kUpPitch<RT> + t * 32 + 8 * q);
+  while (o0 < end) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int o = o0 + 128 * u + 8 * q;
+#pragma unroll
+      for (int s = 0; s < NSUB; ++s) {
+        f32x4 d[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          d[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int t = 0; t < RT; ++t) d[j] = mfma16(wf[u][j][t], pf[s][t], d[j]);
+        }
+        const float v[8] = {d[0][0], d[0][1], d[0][2], d[0][3], d[1][0], d[1][1], d[1][2], d[1][3]};
+        if (o < end && s * 16 + row < tile.count) st16(yr[s] + o, lora_add8(b[u][s], v));
+      }
+    }
+    o0 += 128 * UN;
+    if (o0 < end) load(o0);
   }
 }
 
+// Runs of 32 columns that a wave loads at once: up to 24 vectors of 16 bytes.
+template <int RT>
+constexpr int kUpRuns = RT == 1 ? 4 : RT <= 4 ? 2 : 1;
+
 template <int RT>
 __global__ __launch_bounds__(256) void lora_up_kernel(LoraUp a, LoraPlan plan) {
-  __shared__ __align__(16) uint16_t s_terms[2][64 * kUpPitch<RT>];
-  if (!plan.valid()) return;
+  __shared__ __align__(16) uint16_t s_terms[64 * kUpPitch<RT>];
   const int blocks = a.first[a.parts], ti = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
-  if (ti >= plan.head[3]) return;
-  const LoraTile tile = plan.tiles[ti];
+  int tok[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
+  const LoraTile tile = plan.tile(plan.tiles, ti, 3);
+  if (tile.count == 0) return;
   int part = 0;
   while (part + 1 < a.parts && cbk >= a.first[part + 1]) ++part;
   const int cb = (cbk - a.first[part]) * a.span;
   const bool keep = a.P != nullptr && cb == 0;
-  if (tile.adapter >= plan.n) {
-    lora_copy(a, plan, tile, a.off[part] + cb, min(a.span, a.width[part] - cb), part * a.r, keep ? a.r : 0);
-    return;
-  }
-  const int subs = (tile.count + 15) / 16, nsub = subs == 3 ? 4 : subs;
-  lora_stage<RT>(a, plan, tile, 0, nsub * 16, part * a.r, 0, a.r, keep, s_terms[0], s_terms[1]);
-  __syncthreads();
-  if (nsub == 1)
-    lora_up_body<RT, 1>(a, plan, tile, part, cb, s_terms[0], s_terms[1]);
-  else if (nsub == 2)
-    lora_up_body<RT, 2>(a, plan, tile, part, cb, s_terms[0], s_terms[1]);
+  if (tile.adapter >= plan.n)
+    lora_copy(a, plan, tile, ti, a.off[part] + cb, min(a.span, a.width[part] - cb), part * a.r, keep ? a.r : 0);
+  else if (tile.count <= 16)
+    lora_up_body<RT, 1, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
+  else if (tile.count <= 32)
+    lora_up_body<RT, 2, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
   else
-    lora_up_body<RT, 4>(a, plan, tile, part, cb, s_terms[0], s_terms[1]);
+    lora_up_body<RT, 4, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
 }
+
+constexpr int kUpTCols = 512;  // columns per block, 128 per wave
 
 // dX = base + Q A.  A's rows are ranks, so a lane loads eight ranks of eight
 // columns and transposes them in registers; eight instructions then give a
-// lane four runs of eight consecutive columns (32 apart) of one token.
-constexpr int kUpTRanks = 64;   // ranks staged at a time
-constexpr int kUpTCols = 512;   // columns per block, 128 per wave
-
-__global__ __launch_bounds__(256) void lora_up_t_kernel(LoraUp a, int d_in, LoraPlan plan) {
-  constexpr int RT = kUpTRanks / 16, NS = 2;
-  __shared__ __align__(16) uint16_t s_terms[2][16 * NS * kUpPitch<RT>];
-  if (!plan.valid()) return;
-  const int blocks = (d_in + kUpTCols - 1) / kUpTCols, ti = blockIdx.x / blocks, cb = blockIdx.x % blocks * kUpTCols;
-  if (ti >= plan.head[3]) return;
-  const LoraTile tile = plan.tiles[ti];
-  if (tile.adapter >= plan.n) {
-    lora_copy(a, plan, tile, cb, min(kUpTCols, d_in - cb), 0, 0);
-    return;
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
-  const int c0 = cb + 128 * wave;
+// lane four runs of eight consecutive columns (32 apart) of one token.  Q's terms come as
+// lora_terms_kernel left them.
+template <int NSUB>
+__device__ __forceinline__ void lora_up_t_body(const LoraUp& a, const uint16_t* Qn, int blocksQ, int d_in,
+                                               const LoraTile& tile, int ti, const int (&tok)[4], int c0) {
+  const int lane = threadIdx.x & 63, row = lane & 15, q = lane >> 4;
   const int wc = c0 + 8 * (4 * (row & 3) + (row >> 2));  // row 4 q + i of the products: columns 32 i + 8 q + c
-  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + wc;
-  for (int t0 = 0; t0 < tile.count; t0 += 16 * NS) {
-    uint16_t* yr[NS];
-    u32x4 b[NS][4];
+  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + min(wc, d_in - 8);
+  const uint16_t* qn = Qn + (int64_t(ti) * kLoraTile + row) * blocksQ * 32 + 8 * q;
+  f32x4 acc[NSUB][8];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int64_t tok = plan.order[tile.pos + min(t0 + s * 16 + row, tile.count - 1)];
-      yr[s] = a.Y + tok * a.ldy + c0 + 8 * q;
-      const uint16_t* br = a.base + tok * a.ld_base + c0 + 8 * q;
+  for (int s = 0; s < NSUB; ++s)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) b[s][i] = c0 + 32 * i + 8 * q < d_in ? ld16(br + 32 * i) : zero16();
-    }
-    f32x4 acc[NS][8];
+    for (int c = 0; c < 8; ++c) acc[s][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  u32x4 v[8], b[2][4];
+  auto load_w = [&](int t) {
+    const int k = 16 * t + 8 * (q & 1);
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int j = 0; j < 8; ++j) v[j] = k < a.R ? ld16(w + int64_t(k + j) * d_in) : zero16();
+  };
+  auto load_base = [&](int s) {
+    const uint16_t* br = a.base + int64_t(tok[s]) * a.ld_base + c0 + 8 * q;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) acc[s][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int r0 = 0; r0 < a.r; r0 += kUpTRanks) {
-      __syncthreads();
-      lora_stage<RT>(a, plan, tile, t0, 16 * NS, 0, r0, a.r, false, s_terms[0], s_terms[1]);
-      __syncthreads();
-      const int nt = (min(a.r - r0, kUpTRanks) + 15) / 16;
-      for (int t = 0; t < nt; ++t) {
-        const int k = r0 + 16 * t + 8 * (q & 1);
-        u32x4 v[8], wf[8];
+    for (int i = 0; i < 4; ++i) b[s & 1][i] = c0 + 32 * i + 8 * q < d_in ? ld16(br + 32 * i) : zero16();
+  };
+  load_w(0);
+  load_base(0);
+  if (NSUB > 1) load_base(1);
+  for (int t = 0; t < blocksQ; ++t) {
+    u32x4 wf[8], pf[NSUB];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = k < a.r && wc < d_in ? ld16(w + int64_t(k + j) * d_in) : zero16();
-        transpose8x8_b16(v, wf);
+    for (int s = 0; s < NSUB; ++s) pf[s] = ld16(qn + (int64_t(s) * 16 * blocksQ + t) * 32);
+    transpose8x8_b16(v, wf);
+    if (t + 1 < blocksQ) load_w(t + 1);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const u32x4 pf = ld16(s_terms[q >> 1] + (s * 16 + row) * kUpPitch<RT> + 16 * t + 8 * (q & 1));
+    for (int s = 0; s < NSUB; ++s)
 #pragma unroll
-          for (int c = 0; c < 8; ++c) acc[s][c] = mfma16(wf[c], pf, acc[s][c]);
-        }
-      }
-    }
-#pragma unroll
-    for (int s = 0; s < NS; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float v[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = acc[s][c][i];
-        if (c0 + 32 * i + 8 * q < d_in && t0 + s * 16 + row < tile.count) st16(yr[s] + 32 * i, lora_add8(b[s][i], v));
-      }
+      for (int c = 0; c < 8; ++c) acc[s][c] = mfma16(wf[c], pf[s], acc[s][c]);
   }
+#pragma unroll
+  for (int s = 0; s < NSUB; ++s) {
+    uint16_t* yr = a.Y + int64_t(tok[s]) * a.ldy + c0 + 8 * q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float d[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) d[c] = acc[s][c][i];
+      if (c0 + 32 * i + 8 * q < d_in && s * 16 + row < tile.count) st16(yr + 32 * i, lora_add8(b[s & 1][i], d));
+    }
+    if (s + 2 < NSUB) load_base(s + 2);
+  }
+}
+
+__global__ __launch_bounds__(256) void lora_up_t_kernel(LoraUp a, const uint16_t* Qn, int blocksQ, int d_in,
+                                                        LoraPlan plan) {
+  const int blocks = (d_in + kUpTCols - 1) / kUpTCols, ti = blockIdx.x / blocks, cb = blockIdx.x % blocks * kUpTCols;
+  int tok[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
+  const LoraTile tile = plan.tile(plan.tiles, ti, 3);
+  if (tile.count == 0) return;
+  const int c0 = cb + 128 * (threadIdx.x >> 6);
+  if (tile.adapter >= plan.n)
+    lora_copy(a, plan, tile, ti, cb, min(kUpTCols, d_in - cb), 0, 0);
+  else if (c0 >= d_in)
+    return;
+  else if (tile.count <= 16)
+    lora_up_t_body<1>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
+  else if (tile.count <= 32)
+    lora_up_t_body<2>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
+  else
+    lora_up_t_body<4>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
 }
 
 // ---------------------------------------------------------------- products with the tokens contracted
@@ -547,96 +692,109 @@ __global__ __launch_bounds__(256) void lora_up_t_kernel(LoraUp a, int d_in, Lora
 struct LoraGrad {
   const uint16_t* X;  // the tall matrix
   int64_t ldx;
-  const float* low;  // [T, R]: P in the tokens' order, or Q in the plan's
-  int R, r;          // ranks of a part (R for dA)
+  const uint16_t* terms;  // fragments of Q or P (lora_terms_kernel)
+  int tblocks;            // their blocks of 16 ranks, all parts
+  int pblocks;            // of one part
+  int r;                  // ranks of a part (R for dA)
   const float* scale;
-  float* out;     // [n, ranks, cols] (dA) or [n, cols, r] (dB)
+  float* out;       // [n, ranks, cols] (dA) or [n, cols, r] (dB)
   int64_t ostride;  // elements per adapter
   int ocols;        // all columns of the tall matrix
-  float* part;    // the same, per gradient tile
-  int chunks, parts;
+  float* part;      // the same, per gradient tile
+  int parts;
   int off[kLoraMaxParts], width[kLoraMaxParts], first[kLoraMaxParts + 1];
 };
 
+// Stages in LDS: two blocks per CU at 64 ranks (20 KiB a stage), three at 16 (11 KiB).
+template <int RT>
+constexpr int kGradStages = RT == 4 ? 3 : 4;
+
+// 16 bytes per lane from memory into LDS at lds + 16 lane (uniform), without a register between.
+__device__ __forceinline__ void lora_dma16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+
 // One block sums the products of up to 512 tokens of one adapter for 128
-// columns and 16 RT ranks, each wave over 32 of every 128 tokens.  A lane loads eight
-// tokens of eight columns and transposes them in registers, so that the tokens become
-// the contracted index without a trip through LDS.  An adapter with
-// one tile of tokens is done; others leave partial sums.
+// columns and 16 RT ranks.  A stage of the pipeline is 32 tokens: their rows
+// of the tall matrix and the terms' fragments are copied into LDS two or three stages ahead, and
+// the rows come back transposed, so that the tokens become the contracted
+// index.  The waves split ranks and columns, never tokens, so no sum crosses a wave.
+// An adapter with one gradient tile is done; others leave partial sums.
 template <int RT, bool DB>
 __global__ __launch_bounds__(256) void lora_grad_kernel(LoraGrad a, LoraPlan plan) {
-  __shared__ float s_red[4 * 128 * 17];
-  if (!plan.valid()) return;
+  constexpr int NS = kGradStages<RT>;
+  constexpr int NC = 2 * RT;                  // 16-column fragments per wave: 128 RT / 4 columns
+  constexpr int COPIES = 8 + 3 * RT;          // 1 KiB each: 4 rows of 128 columns, or one fragment
+  constexpr int PER = (COPIES + 3) / 4;       // per wave
+  __shared__ u32x4 s_stage[NS][COPIES * 64];
+  __shared__ int s_tok[512];
   const int blocks = a.first[a.parts], gi = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
-  if (gi >= plan.head[4]) return;
-  const LoraTile tile = plan.gtiles[gi];
+  const LoraTile tile = plan.tile(plan.gtiles, gi, 4);
+  if (tile.count == 0) return;
   int part = 0;
   while (part + 1 < a.parts && cbk >= a.first[part + 1]) ++part;
   const int cb = (cbk - a.first[part]) * kLoraGradCols, width = a.width[part];
-  const int r0 = blockIdx.y * 16 * RT, nr = min(16 * RT, a.r - r0);
+  const int rb0 = blockIdx.y * RT;  // first block of 16 ranks within the part
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
-  const int cols = cb + 8 * row;
-  const uint16_t* x = a.X + a.off[part] + cols;
-  const float* low = a.low + (DB ? part * a.r : 0) + r0 + row;
-  f32x4 acc[8][RT];
+  const int steps = (tile.count + 31) / 32;
+  for (int i = threadIdx.x; i < 32 * steps; i += 256) s_tok[i] = plan.tokens[tile.pos * kLoraTile + i];
+  __syncthreads();
+  const uint32_t lds = lds_addr(s_stage);
+  const uint16_t* x = a.X + a.off[part] + cb;
+  const uint16_t* terms = a.terms + (int64_t(tile.pos) * 2 * a.tblocks + part * a.pblocks) * (3 * 512) + lane * 8;
+  auto issue = [&](int step) {
+    const uint32_t at = lds + uint32_t(step % NS) * (COPIES * 1024);
 #pragma unroll
-  for (int c = 0; c < 8; ++c)
-#pragma unroll
-    for (int t = 0; t < RT; ++t) acc[c][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int tb = 32 * wave; tb < tile.count; tb += 128) {
-    u32x4 v[8], xf[8];
-    float l[RT][8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = tb + 8 * q + j;
-      const bool on = t < tile.count;
-      const int p = tile.pos + min(t, tile.count - 1);
-      const int64_t tok = plan.order[p];
-      v[j] = on && cols < width ? ld16(x + tok * a.ldx) : zero16();
-      const float* lr = low + (DB ? tok : int64_t(p)) * a.R;
-#pragma unroll
-      for (int u = 0; u < RT; ++u) l[u][j] = on && 16 * u + row < nr ? lr[16 * u] : 0.0f;
-    }
-    transpose8x8_b16(v, xf);
-#pragma unroll
-    for (int u = 0; u < RT; ++u) {
-      u32x4 f[3];
-      float rest[8];
-      lora_terms(l[u], f[0], f[1]);
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        rest[2 * p] = lora_rest(lora_rest(l[u][2 * p], f[0][p] & 0xffffu), f[1][p] & 0xffffu);
-        rest[2 * p + 1] = lora_rest(lora_rest(l[u][2 * p + 1], f[0][p] >> 16), f[1][p] >> 16);
-        f[2][p] = pack_bf16x2(rest[2 * p], rest[2 * p + 1]);
+    for (int i = 0; i < PER; ++i) {
+      const int c = min(wave + 4 * i, COPIES - 1);  // uniform; a wave with fewer repeats the last
+      const void* p;
+      if (c < 8) {
+        int r, chunk;
+        mn_dma_target<128>(c * 64 + lane, r, chunk);
+        p = x + int64_t(s_tok[32 * step + r]) * a.ldx + min(8 * chunk, width - cb - 8);
+      } else {
+        const int f = c - 8, rb = min(rb0 + f / 3, a.pblocks - 1);
+        p = terms + (int64_t(step) * a.tblocks + rb) * (3 * 512) + (f % 3) * 512;
       }
+      lora_dma16(p, __builtin_amdgcn_readfirstlane(at + uint32_t(c) * 1024));
+    }
+  };
+  f32x4 acc[NC];
 #pragma unroll
-      for (int m = 0; m < 3; ++m)
+  for (int c = 0; c < NC; ++c) acc[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int rb = wave % RT, cw = wave / RT * (16 * NC);  // this wave's ranks and columns
+  for (int s = 0; s < NS - 1 && s < steps; ++s) issue(s);
+  for (int s = 0; s < steps; ++s) {
+    // stage s has landed, and the stage that is filled next has been read by every wave
+    wait_stages<PER>(min(steps - 1 - s, NS - 2));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    block_sync();
+    if (s + NS - 1 < steps) issue(s + NS - 1);
+    const u32x4* st = s_stage[s % NS];
+    u32x4 f[3];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[c][u] = mfma16(xf[c], f[m], acc[c][u]);
+    for (int m = 0; m < 3; ++m) f[m] = st[(8 + 3 * rb + m) * 64 + lane];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const u32x4 xf = mn_frag<128>(st, cw + 16 * c, lane);
+#pragma unroll
+      for (int m = 0; m < 3; ++m) acc[c] = mfma16(xf, f[m], acc[c]);
     }
   }
+  const int rank = 16 * (rb0 + rb) + row;
+  if (rank >= a.r) return;
   float* out = tile.only ? a.out + tile.adapter * a.ostride : a.part + gi * a.ostride;
   const float scale = DB ? a.scale[tile.adapter] : 1.0f;
-  for (int u = 0; u < RT; ++u) {
-    if (u * 16 >= nr) break;  // uniform
-    __syncthreads();
 #pragma unroll
-    for (int t = 0; t < RT; ++t)
-      if (t == u) {
+  for (int c = 0; c < NC; ++c) {
+    const int col = cw + 16 * c + 4 * q;
+    if (cb + col >= width) continue;
+    const int64_t at = a.off[part] + cb + col;
+    if constexpr (DB) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s_red[(wave * 128 + 8 * (4 * q + i) + c) * 17 + row] = acc[c][t][i];
-      }
-    __syncthreads();
-    for (int e = threadIdx.x; e < 128 * 16; e += 256) {
-      const int c = DB ? e >> 4 : e & 127, k = DB ? e & 15 : e >> 7;
-      const float* p = s_red + c * 17 + k;
-      const float g = scale * ((p[0] + p[128 * 17]) + (p[256 * 17] + p[384 * 17]));
-      if (cb + c < width && u * 16 + k < nr) {
-        const int64_t col = a.off[part] + cb + c, rank = r0 + u * 16 + k;
-        out[DB ? col * a.r + rank : rank * a.ocols + col] = g;
-      }
+      for (int i = 0; i < 4; ++i) out[(at + i) * a.r + rank] = acc[c][i] * scale;
+    } else {
+      *reinterpret_cast<f32x4*>(out + rank * int64_t(a.ocols) + at) = acc[c];
     }
   }
 }
@@ -646,9 +804,8 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraGrad a, LoraPlan pla
 __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float* __restrict__ partA, float* __restrict__ dA,
                                                             int64_t sA, int blocksA, const float* __restrict__ partB,
                                                             float* __restrict__ dB, int64_t sB, LoraPlan plan) {
-  if (!plan.valid()) return;
   const int a = blockIdx.y, g0 = plan.gstart[a], g1 = plan.gstart[a + 1];
-  if (g1 - g0 == 1) return;
+  if (plan.head[0] != kLoraMagic || plan.head[1] != plan.T || plan.head[2] != plan.n || g1 - g0 == 1) return;
   const bool second = int(blockIdx.x) >= blocksA;
   const float* part = second ? partB : partA;
   const int64_t stride = second ? sB : sA;
@@ -666,10 +823,12 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float* __restr
 hipError_t launch_lora_plan(const int* adapter, int T, int n, void* plan, hipStream_t s) {
   const LoraPlanLayout L = lora_plan_layout(T, n);
   int* w = static_cast<int*>(plan);
-  const size_t lds = size_t(kPlanWaves * (n + 1) + 3 * (n + 2)) * sizeof(int);
-  hipLaunchKernelGGL(lora_plan_kernel, dim3(1), dim3(64 * kPlanWaves), lds, s, adapter, T, n, lora_grad_tokens(T), w,
-                     w + L.order, w + L.start, w + L.gstart, reinterpret_cast<LoraTile*>(w + L.tiles),
-                     reinterpret_cast<LoraTile*>(w + L.gtiles));
+  // 16 waves where their counts fit LDS beside the rest
+  const int waves = n <= 1024 ? kPlanMaxWaves : kPlanMaxWaves / 2;
+  const size_t lds = size_t(waves * (n + 1) + 3 * (n + 2)) * sizeof(int);
+  hipLaunchKernelGGL(lora_plan_kernel, dim3(1), dim3(64 * waves), lds, s, adapter, T, n, lora_grad_tokens(T), w,
+                     reinterpret_cast<LoraTile*>(w + L.tiles), w + L.tokens, reinterpret_cast<LoraTile*>(w + L.gtiles),
+                     w + L.gstart);
   return hipGetLastError();
 }
 
@@ -707,7 +866,7 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   d.chunks = (R + 16 * rt - 1) / (16 * rt);
   if (hipError_t e = launch_down<false>(d, pl, tiles, rt, d.chunks, s)) return e;
   LoraUp u = {};
-  u.low = part, u.splits = splits, u.R = R, u.scale = scale;
+  u.part = part, u.splits = splits, u.R = R, u.scale = scale;
   u.W = B, u.wstride = int64_t(z.d_out) * z.r, u.r = z.r;
   u.base = base, u.ld_base = ld_base, u.Y = Y, u.ldy = ldy, u.P = P, u.parts = z.parts;
   // Blocks of 512 columns where that gives every CU a few; narrower ones below.
@@ -727,8 +886,9 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
 }
 
 template <bool DB>
-static hipError_t launch_grad(const LoraGrad& a, const LoraPlan& plan, int gtiles, int rt, hipStream_t s) {
-  const dim3 grid(unsigned(gtiles) * unsigned(a.first[a.parts]), unsigned(a.chunks)), block(256);
+static hipError_t launch_grad(const LoraGrad& a, const LoraPlan& plan, int gtiles, hipStream_t s) {
+  const int rt = rank_tiles(a.r);
+  const dim3 grid(unsigned(gtiles) * unsigned(a.first[a.parts]), unsigned((a.r + 16 * rt - 1) / (16 * rt))), block(256);
   switch (rt) {
     case 1: hipLaunchKernelGGL((lora_grad_kernel<1, DB>), grid, block, 0, s, a, plan); break;
     case 2: hipLaunchKernelGGL((lora_grad_kernel<2, DB>), grid, block, 0, s, a, plan); break;
@@ -759,36 +919,37 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
     const int rt = rank_tiles(z.r);
     d.chunks = (z.r + 16 * rt - 1) / (16 * rt);
     if ((e = launch_down<true>(d, pl, tiles, rt, d.chunks * z.parts, s))) return e;
-    hipLaunchKernelGGL(lora_sum_kernel, dim3(tiles), dim3(256), 0, s, w.part, splits, R, scale, pl, w.Q);
-    if ((e = hipGetLastError())) return e;
   }
+  LoraTerms m = {};
+  m.part = w.part, m.splits = splits, m.R = R, m.scale = scale, m.P = P, m.r = z.r, m.parts = z.parts;
+  m.Qn = dX ? w.Qn : nullptr, m.Qt = dA ? w.Qt : nullptr, m.Pt = w.Pt;
+  m.blocksQ = dX || dA ? (R + 15) / 16 : 0, m.blocksP = dB ? z.parts * ((z.r + 15) / 16) : 0;
+  hipLaunchKernelGGL(lora_terms_kernel, dim3(unsigned(tiles) * unsigned(m.blocksQ + m.blocksP)), dim3(256), 0, s, m, pl);
+  if ((e = hipGetLastError())) return e;
   if (dX) {
     LoraUp u = {};
-    u.low = w.Q, u.splits = 1, u.R = R, u.W = A, u.wstride = int64_t(R) * z.d_in, u.r = R;
-    u.base = base, u.ld_base = ld_base, u.Y = dX, u.ldy = lddx, u.parts = 1;
+    u.R = R, u.W = A, u.wstride = int64_t(R) * z.d_in, u.base = base, u.ld_base = ld_base, u.Y = dX, u.ldy = lddx;
     const int blocks = (z.d_in + kUpTCols - 1) / kUpTCols;
-    hipLaunchKernelGGL(lora_up_t_kernel, dim3(unsigned(tiles) * unsigned(blocks)), dim3(256), 0, s, u, z.d_in, pl);
+    hipLaunchKernelGGL(lora_up_t_kernel, dim3(unsigned(tiles) * unsigned(blocks)), dim3(256), 0, s, u, w.Qn, m.blocksQ,
+                       z.d_in, pl);
     if ((e = hipGetLastError())) return e;
   }
   LoraGrad g = {};
   if (dA) {
-    g.X = X, g.ldx = ldx, g.low = w.Q, g.R = R, g.r = R, g.out = dA, g.ostride = int64_t(R) * z.d_in, g.ocols = z.d_in;
-    g.part = w.partA, g.parts = 1, g.width[0] = z.d_in;
+    g.X = X, g.ldx = ldx, g.terms = w.Qt, g.tblocks = g.pblocks = m.blocksQ, g.r = R;
+    g.out = dA, g.ostride = int64_t(R) * z.d_in, g.ocols = z.d_in, g.part = w.partA, g.parts = 1, g.width[0] = z.d_in;
     g.first[1] = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
-    const int rt = rank_tiles(R);
-    g.chunks = (R + 16 * rt - 1) / (16 * rt);
-    if ((e = launch_grad<false>(g, pl, gtiles, rt, s))) return e;
+    if ((e = launch_grad<false>(g, pl, gtiles, s))) return e;
   }
   if (dB) {
-    g.X = dY, g.ldx = lddy, g.low = P, g.R = R, g.r = z.r, g.scale = scale, g.out = dB;
-    g.ostride = int64_t(z.d_out) * z.r, g.ocols = z.d_out, g.part = w.partB, g.parts = z.parts;
+    g.X = dY, g.ldx = lddy, g.terms = w.Pt, g.tblocks = m.blocksP, g.pblocks = m.blocksP / z.parts, g.r = z.r;
+    g.scale = scale, g.out = dB, g.ostride = int64_t(z.d_out) * z.r, g.ocols = z.d_out, g.part = w.partB;
+    g.parts = z.parts;
     for (int p = 0; p < z.parts; ++p) {
       g.off[p] = off[p], g.width[p] = z.widths[p];
       g.first[p + 1] = g.first[p] + (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
     }
-    const int rt = rank_tiles(z.r);
-    g.chunks = (z.r + 16 * rt - 1) / (16 * rt);
-    if ((e = launch_grad<true>(g, pl, gtiles, rt, s))) return e;
+    if ((e = launch_grad<true>(g, pl, gtiles, s))) return e;
   }
   if (dA || dB) {
     const int64_t sA = int64_t(R) * z.d_in, sB = int64_t(z.d_out) * z.r;
