@@ -203,146 +203,207 @@ struct LoraDown {
   int chunks;                                    // blocks of 16 RT ranks per part
 };
 
-// part[s][p][c] = sum over split s's K range of X[token p][k] W[c][k].  A
-// block takes a tile of up to 64 tokens; its waves take 128 of every 512 k, so
-// that an adapter's fragment is loaded once and used for all four 16-token
-// fragments, and add up through LDS.  Fragments come straight from memory into
-// registers, four steps of 32 k ahead of their use.  B is contracted over its
-// rows: 128 of them go through LDS and come back transposed.
-template <int RT, bool BMAJOR, int NSUB>
-__device__ __forceinline__ void lora_down_body(const LoraDown& a, const LoraTile& tile, const LoraPlan& plan,
-                                               const int (&tok)[4], int split, int chunk, int part, float* s_red,
-                                               u32x4* s_w) {
+// 16 bytes per lane from memory into LDS at lds + 16 lane (uniform), without a register between.
+__device__ __forceinline__ void lora_dma16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
+}
+
+// Fragment of 16 columns with the rows contracted, from rows of `pitch` bytes in LDS: the lane's column is
+// col0 + lane % 16 and its k rows 8 (lane / 16) .. + 7.  The 16-lane group q reads rows 8 q + (lane % 16) / 4 and + 4.
+__device__ __forceinline__ u32x4 lora_tr_frag(const char* base, int pitch, int col0, int lane) {
+  const int row = lane & 15, q = lane >> 4;
+  const char* b = base + (8 * q + (row >> 2)) * pitch + col0 * 2 + 8 * (row & 3);
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)b);
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(b + 4 * pitch));
+  u32x4 f;
+  __builtin_memcpy(&f, &lo, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+  return f;
+}
+
+constexpr int kDownK = 64;  // contraction length per stage
+// 16-byte slots of LDS: four stages of 64 tokens and 16 RT ranks.
+template <int RT>
+constexpr int kDownSlots = 4 * (8 + 2 * RT) * 64;
+
+// part[s][p][c] = sum over split s's K range of X[token p][k] W[c][k], for a
+// tile of 17 to 64 tokens: 64 k of the tokens' rows and of the adapter are copied into LDS three stages ahead;
+// each wave takes 16 tokens and all ranks.  B is contracted over its rows,
+// which come back transposed.
+template <int RT, bool BMAJOR>
+__device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile& tile, const int* tokens, int k0,
+                                               int k1, int col0, int r0, int nr, float* out, u32x4* s_mem) {
+  constexpr int NS = 4, COPIES = 8 + 2 * RT, PER = (COPIES + 3) / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
-  const int r0 = chunk * 16 * RT, nr = min(16 * RT, a.wrows - r0);
-  const int col0 = BMAJOR ? a.off[part] : 0, K = BMAJOR ? a.width[part] : a.K;
-  const int k0 = split * a.slice, k1 = min(k0 + a.slice, K);
-  const uint16_t* xr[NSUB];
-#pragma unroll
-  for (int s = 0; s < NSUB; ++s) xr[s] = a.X + int64_t(tok[s]) * a.ldx + col0;
+  const uint32_t lds = lds_addr(s_mem);
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride;
-  f32x4 acc[NSUB][RT];
+  // Copy c < 8: 32 k (half c / 4) of 16 tokens; then the adapter's ranks of both halves, or rows of B.
+  const char* src[PER];
+  int kl[PER];  // k within the stage of this lane's 16 bytes
 #pragma unroll
-  for (int s = 0; s < NSUB; ++s)
-#pragma unroll
-    for (int t = 0; t < RT; ++t) acc[s][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  u32x4 x[NSUB][4];
-  // Past the range's end a row's last values stand in, against zeros of the adapter.
-  auto load_x = [&](int kw, int j) {
-    const int k = min(kw + 32 * j + 8 * q, k1 - 8);
-#pragma unroll
-    for (int s = 0; s < NSUB; ++s) x[s][j] = ld16(xr[s] + k);
-  };
-  if (k0 < k1) {
-    if constexpr (!BMAJOR) {
-      u32x4 wf[RT][4];
-      const uint16_t* wr[RT];
-#pragma unroll
-      for (int t = 0; t < RT; ++t) wr[t] = w + int64_t(r0 + min(t * 16 + row, nr - 1)) * K;
-      auto load_w = [&](int kw, int j) {
-        const int k = kw + 32 * j + 8 * q;
-#pragma unroll
-        for (int t = 0; t < RT; ++t) wf[t][j] = ld16(wr[t] + min(k, k1 - 8));
-      };
-#pragma unroll
-      for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
-      for (int kb = k0; kb < k1; kb += kLoraSlice) {
-        const int kw = kb + wave * 128;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool in = kw + 32 * j + 8 * q < k1;
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const u32x4 f = in ? wf[t][j] : zero16();
-#pragma unroll
-            for (int s = 0; s < NSUB; ++s) acc[s][t] = mfma16(x[s][j], f, acc[s][t]);
-          }
-          if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
-        }
-      }
+  for (int i = 0; i < PER; ++i) {
+    const int c = min(wave + 4 * i, COPIES - 1);  // a wave with fewer repeats the last
+    int r, chunk;
+    if (c < 8) {
+      km_dma_target((c & 3) * 64 + lane, r, chunk);
+      kl[i] = 32 * (c >> 2) + 8 * chunk;
+      src[i] = reinterpret_cast<const char*>(a.X + int64_t(tokens[r]) * a.ldx + col0);
+    } else if (!BMAJOR) {
+      const int f = c - 8;
+      km_dma_target((f % RT) * 64 + lane, r, chunk);
+      kl[i] = 32 * (f / RT) + 8 * chunk;
+      src[i] = reinterpret_cast<const char*>(w + int64_t(r0 + min(r, nr - 1)) * a.K);
     } else {
-      constexpr int CH = 2 * RT;  // 16-byte chunks per row of 16 RT ranks
-      w += int64_t(col0) * a.wrows + r0;
-      u32x4* sw = s_w + wave * 128 * CH;
-      u32x4 v[CH * 2];
-      auto load_w = [&](int kw) {
+      const int e = (c - 8) * 64 + lane;
+      kl[i] = e / (2 * RT);
+      src[i] = reinterpret_cast<const char*>(w + int64_t(col0) * a.wrows + r0 + min(8 * (e % (2 * RT)), nr - 8));
+    }
+  }
+  // Past the range's end the last values stand in, against zeros of the adapter.
+  auto issue = [&](int step) {
+    const uint32_t at = lds + uint32_t(step % NS) * (COPIES * 1024);
 #pragma unroll
-        for (int i = 0; i < CH * 2; ++i) {
-          const int e = i * 64 + lane, k = min(kw + e / CH, k1 - 1), c = min(8 * (e % CH), nr - 8);
-          v[i] = ld16(w + int64_t(k) * a.wrows + c);
-        }
-      };
-      load_w(k0 + wave * 128);
+    for (int i = 0; i < PER; ++i) {
+      const int c = min(wave + 4 * i, COPIES - 1), k = k0 + step * kDownK + kl[i];
+      const char* p = BMAJOR && c >= 8 ? src[i] + int64_t(min(k, k1 - 1)) * a.wrows * 2 : src[i] + int64_t(min(k, k1 - 8)) * 2;
+      lora_dma16(p, __builtin_amdgcn_readfirstlane(at + uint32_t(c) * 1024));
+    }
+  };
+  f32x4 acc[RT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j);
-      for (int kb = k0; kb < k1; kb += kLoraSlice) {
-        const int kw = kb + wave * 128;
-        __builtin_amdgcn_wave_barrier();
+  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int steps = (k1 - k0 + kDownK - 1) / kDownK;
+  for (int s = 0; s < NS - 1 && s < steps; ++s) issue(s);
+  for (int s = 0; s < steps; ++s) {
+    wait_stages<PER>(min(steps - 1 - s, NS - 2));
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    block_sync();
+    if (s + NS - 1 < steps) issue(s + NS - 1);
+    const u32x4* st = s_mem + s % NS * (COPIES * 64);
 #pragma unroll
-        for (int i = 0; i < CH * 2; ++i) {
-          const int k = kw + (i * 64 + lane) / CH;
-          sw[i * 64 + lane] = k < k1 ? v[i] : zero16();
-        }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        if (kb + kLoraSlice < k1) load_w(kw + kLoraSlice);
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 x = km_frag(st + h * 256, 16 * wave, lane);
+      const bool in = k0 + s * kDownK + 32 * h + 8 * q < k1;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            // the 16-lane group q reads rows 8 q + (row / 4) and + 4 of the 32, columns 4 (row % 4) .. + 3
-            const char* b =
-                reinterpret_cast<const char*>(sw) + (32 * j + 8 * q + (row >> 2)) * (CH * 16) + t * 32 + 8 * (row & 3);
-            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)b);
-            const i16x4 hi =
-                __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(b + 4 * CH * 16));
-            u32x4 f;
-            __builtin_memcpy(&f, &lo, 8);
-            __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
-#pragma unroll
-            for (int s = 0; s < NSUB; ++s) acc[s][t] = mfma16(x[s][j], f, acc[s][t]);
-          }
-          if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j);
-        }
+      for (int t = 0; t < RT; ++t) {
+        u32x4 f = BMAJOR ? lora_tr_frag(reinterpret_cast<const char*>(st + 512) + 32 * h * (32 * RT), 32 * RT, 16 * t, lane)
+                         : km_frag(st + 512 + h * 64 * RT, 16 * t, lane);
+        f = in ? f : zero16();
+        acc[t] = mfma16(x, f, acc[t]);
       }
     }
   }
-  float* out = a.part + (int64_t(split) * plan.T + tile.pos) * a.R + part * a.wrows + r0;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    if (t * 16 >= nr) break;  // uniform
-    if (t > 0) __syncthreads();
+  for (int t = 0; t < RT; ++t)
 #pragma unroll
-    for (int s = 0; s < NSUB; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s_red[(wave * 64 + s * 16 + 4 * q + i) * 17 + row] = acc[s][t][i];
-    __syncthreads();
-    for (int e = threadIdx.x; e < NSUB * 256; e += 256) {
-      const int i = e >> 4, c = e & 15;
-      const float v =
-          (s_red[i * 17 + c] + s_red[(64 + i) * 17 + c]) + (s_red[(128 + i) * 17 + c] + s_red[(192 + i) * 17 + c]);
-      if (i < tile.count && t * 16 + c < nr) out[int64_t(i) * a.R + t * 16 + c] = v;
+    for (int i = 0; i < 4; ++i) {
+      const int tok = 16 * wave + 4 * q + i;
+      if (tok < tile.count && t * 16 + row < nr) out[int64_t(tok) * a.R + t * 16 + row] = acc[t][i];
     }
+}
+
+// The same for a tile of up to 16 tokens, where the adapter is the operand that
+// counts: the waves take 128 of every 512 k and add up through LDS, and
+// fragments come straight from memory into registers, four steps of 32 k ahead.
+template <int RT, bool BMAJOR>
+__device__ __forceinline__ void lora_down_few(const LoraDown& a, const LoraTile& tile, int tok, int k0, int k1, int col0,
+                                              int r0, int nr, float* out, u32x4* s_mem) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
+  const uint16_t* xr = a.X + int64_t(tok) * a.ldx + col0;
+  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride;
+  f32x4 acc[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  u32x4 x[4];
+  auto load_x = [&](int kw, int j) { x[j] = ld16(xr + min(kw + 32 * j + 8 * q, k1 - 8)); };
+  if constexpr (!BMAJOR) {
+    u32x4 wf[RT][4];
+    const uint16_t* wr[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) wr[t] = w + int64_t(r0 + min(t * 16 + row, nr - 1)) * a.K;
+    auto load_w = [&](int kw, int j) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) wf[t][j] = ld16(wr[t] + min(kw + 32 * j + 8 * q, k1 - 8));
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
+    for (int kb = k0; kb < k1; kb += kLoraSlice) {
+      const int kw = kb + wave * 128;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool in = kw + 32 * j + 8 * q < k1;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) acc[t] = mfma16(x[j], in ? wf[t][j] : zero16(), acc[t]);
+        if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
+      }
+    }
+  } else {
+    constexpr int CH = 2 * RT;  // 16-byte chunks per row of 16 RT ranks; a wave's 32 rows in LDS at a time
+    w += int64_t(col0) * a.wrows + r0;
+    u32x4* sw = s_mem + wave * 32 * CH;
+    u32x4 v[RT][4];
+    auto load_w = [&](int kw, int j) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const int e = i * 64 + lane;
+        v[i][j] = ld16(w + int64_t(min(kw + 32 * j + e / CH, k1 - 1)) * a.wrows + min(8 * (e % CH), nr - 8));
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
+    for (int kb = k0; kb < k1; kb += kLoraSlice) {
+      const int kw = kb + wave * 128;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i) sw[i * 64 + lane] = v[i][j];
+        __syncthreads();
+        const bool in = kw + 32 * j + 8 * q < k1;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          const u32x4 f = lora_tr_frag(reinterpret_cast<const char*>(sw), 32 * RT, 16 * t, lane);
+          acc[t] = mfma16(x[j], in ? f : zero16(), acc[t]);
+        }
+        if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
+      }
+    }
+  }
+  float* s_red = reinterpret_cast<float*>(s_mem);  // [4 waves][16 tokens][16 RT ranks, 1 spare]
+  constexpr int P = 16 * RT + 1;
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_red[(wave * 16 + 4 * q + i) * P + t * 16 + row] = acc[t][i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < 256 * RT; e += 256) {
+    const int i = e / (16 * RT), c = e % (16 * RT);
+    const float v = (s_red[i * P + c] + s_red[(16 + i) * P + c]) + (s_red[(32 + i) * P + c] + s_red[(48 + i) * P + c]);
+    if (i < tile.count && c < nr) out[int64_t(i) * a.R + c] = v;
   }
 }
 
 template <int RT, bool BMAJOR>
-__global__ __launch_bounds__(256) void lora_down_kernel(LoraDown a, LoraPlan plan) {
-  __shared__ float s_red[256 * 17];
-  __shared__ u32x4 s_w[BMAJOR ? 4 * 128 * 2 * RT : 1];
+__global__ __launch_bounds__(256, 2) void lora_down_kernel(LoraDown a, LoraPlan plan) {
+  __shared__ u32x4 s_mem[kDownSlots<RT>];
   const int split = blockIdx.x % a.splits, ti = blockIdx.x / a.splits;
-  int tok[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
+  const int* tokens = plan.tokens + ti * kLoraTile;
+  const int tok = tokens[threadIdx.x & 15];
   const LoraTile tile = plan.tile(plan.tiles, ti, 3);
   if (tile.count == 0 || tile.adapter >= plan.n) return;
   const int chunk = blockIdx.y % a.chunks, part = BMAJOR ? blockIdx.y / a.chunks : 0;
-  if (tile.count <= 16)
-    lora_down_body<RT, BMAJOR, 1>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
-  else if (tile.count <= 32)
-    lora_down_body<RT, BMAJOR, 2>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
-  else
-    lora_down_body<RT, BMAJOR, 4>(a, tile, plan, tok, split, chunk, part, s_red, s_w);
+  const int r0 = chunk * 16 * RT, nr = min(16 * RT, a.wrows - r0);
+  const int col0 = BMAJOR ? a.off[part] : 0, K = BMAJOR ? a.width[part] : a.K;
+  const int k0 = split * a.slice, k1 = min(k0 + a.slice, K);
+  float* out = a.part + (int64_t(split) * plan.T + tile.pos) * a.R + part * a.wrows + r0;
+  if (k0 >= k1) {  // a narrower part than the widest
+    for (int e = threadIdx.x; e < tile.count * nr; e += 256) out[int64_t(e / nr) * a.R + e % nr] = 0.0f;
+  } else if (tile.count <= 16) {
+    lora_down_few<RT, BMAJOR>(a, tile, tok, k0, k1, col0, r0, nr, out, s_mem);
+  } else {
+    lora_down_wide<RT, BMAJOR>(a, tile, tokens, k0, k1, col0, r0, nr, out, s_mem);
+  }
 }
 
 // Sum of the splits' partial sums at p, four values.
@@ -456,6 +517,8 @@ struct LoraUp {
   uint16_t* Y;
   int64_t ldy;
   float* P;  // [T, R] in the tokens' order, or nullptr
+  const uint16_t* Qn;  // dX: Q's terms instead of `part`
+  int blocksQ;
   int parts, span;  // columns per block
   int off[kLoraMaxParts], width[kLoraMaxParts], first[kLoraMaxParts + 1];  // first block of each part
 };
@@ -516,83 +579,170 @@ __device__ __forceinline__ u32x4 lora_add8(const u32x4& b, const float (&d)[8]) 
   return r;
 }
 
-// Y = base + c P B^T.  The matrix product's rows are output columns and its
-// columns tokens, with B's rows dealt so that two instructions leave eight
-// consecutive columns of one token in each lane: base and Y move as 16-byte
-// vectors straight between memory and registers, 64 bytes per token.  One
-// instruction's 32 k hold the two terms of 16 ranks.  A wave loads UN runs of 32
-// columns at once; the first before the ranks are staged.
-template <int RT, int NSUB, int UN>
+// Columns whose weights are in LDS at a time: 32 KiB of them, at most 512 columns.
+template <int RT>
+constexpr int kUpCols = RT == 1 ? 512 : 1024 / RT;
+
+// B's chunk of 8 ranks c of row o is at c ^ up_swizzle(o): the rows that eight lanes read at once then lie in
+// different 16-byte columns.
+template <int RT>
+__device__ __forceinline__ int up_swizzle(int o) {
+  if constexpr (RT == 1)
+    return (o >> 3) & 1;
+  else if constexpr (RT == 2)
+    return ((o >> 1) & 1) | ((o >> 3) & 1) << 1;
+  else
+    return (o & 3) | ((o >> 3) & 1) << 2;
+}
+
+// Y = base + c P B^T, and with TR dX = base + Q A.  The matrix product's rows
+// are output columns and its columns tokens, with the columns dealt so that
+// two instructions leave eight consecutive ones of one token in each lane: base
+// and Y move as 16-byte vectors straight between memory and registers, 64 bytes
+// per token.  One instruction's 32 k hold the two terms of 16 ranks.
+//
+// A block takes 64 tokens and `span` columns; a wave 16 of the tokens and all
+// columns, or a share of the columns where there are fewer tokens.  The weights of kUpCols
+// columns at a time are copied into LDS, which all waves share; A's come back transposed.
+// base is loaded UN runs of 32 columns ahead.  More ranks than fit go in several rounds (MULTI),
+// with the sums of 128 columns held in registers.
+template <int RT, bool TR, bool MULTI>
 __device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int ti,
-                                             const int (&tok)[4], int part, int cb, bool keep, uint16_t* s_terms) {
+                                             int part, int cb, bool keep, int subs, u32x4* s_w, uint16_t* s_terms) {
+  constexpr int COLS = kUpCols<RT>, UN = 4, CPR = COLS / 8, COPIES = COLS * RT / 32;
+  static_assert(!MULTI || (TR && COLS == 32 * UN), "the sums of one round of columns stay in registers");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
-  const int off = a.off[part], width = a.width[part], end = min(cb + a.span, width);
-  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + int64_t(off) * a.r + 8 * (q & 1);
-  const uint16_t* br[NSUB];
-  uint16_t* yr[NSUB];
+  const int off = a.off[part], end = min(cb + a.span, a.width[part]), ranks = TR ? a.R : a.r;
+  const int share = 4 / subs, first = 16 * (wave % subs), o0 = cb + 32 * (wave / subs), stride = 32 * share;
+  const int runs = (end - cb + stride - 1) / stride, per = COLS / stride;  // of a wave: in all, and per weights in LDS
+  const int64_t tok = plan.tokens[ti * kLoraTile + first + row];
+  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + int64_t(off) * (TR ? 1 : a.r);
+  uint16_t* yr = a.Y + tok * a.ldy + off + 8 * q;
+  const uint16_t* br = a.base + tok * a.ld_base + off;
+  const bool on = first + row < tile.count;
+  u32x4 b[UN];
+  auto load_base = [&](int i, int u) {
+    const int o = o0 + stride * i;
+    if (o < end) b[u] = ld16(br + min(o + 8 * q, end - 8));
+  };
 #pragma unroll
-  for (int s = 0; s < NSUB; ++s) {
-    yr[s] = a.Y + int64_t(tok[s]) * a.ldy + off;
-    br[s] = a.base + int64_t(tok[s]) * a.ld_base + off;
-  }
-  u32x4 wf[UN][2][RT], b[UN][NSUB];
-  auto load = [&](int o0) {
+  for (int u = 0; u < UN; ++u) load_base(u, u);
+  const uint32_t lds = lds_addr(s_w);
+  // Weights of columns [c, c + COLS) and ranks [k0, k0 + 16 RT); none past the last column, whose products are
+  // not stored; past the last rank others stand in, against zero terms.
+  auto stage_w = [&](int c, int k0) {
+    block_sync();
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int o = o0 + 128 * u;
-#pragma unroll
-      for (int s = 0; s < NSUB; ++s) b[u][s] = ld16(br[s] + min(o + 8 * q, width - 8));
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int64_t wo = int64_t(min(o + 8 * (row >> 2) + 4 * j + (row & 3), width - 1)) * a.r;
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-          wf[u][j][t] = t * 16 + 8 * (q & 1) < a.r ? ld16(w + wo + t * 16) : zero16();
+    for (int i = 0; i < COPIES / 4; ++i) {
+      const int s = (wave + 4 * i) * 64 + lane;
+      const uint32_t at = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave + 4 * i) * 1024);
+      if constexpr (TR) {
+        const int r = s / CPR, x = s % CPR, chunk = (((x >> 2) ^ (r & 3)) << 2) | (x & 3);
+        const uint16_t* p = w + int64_t(min(k0 + r, ranks - 1)) * a.width[0] + c + 8 * chunk;
+        if (c + 8 * chunk < end) lora_dma16(p, at);
+      } else {
+        const int r = s / (2 * RT), chunk = (s % (2 * RT)) ^ up_swizzle<RT>(r);
+        const uint16_t* p = w + int64_t(c + r) * a.r + min(8 * chunk, ranks - 8);
+        if (c + r < end) lora_dma16(p, at);
       }
     }
   };
-  int o0 = cb + 32 * wave;
-  load(o0);
-  lora_stage<RT>(a, plan, tile, ti, 16 * NSUB, part * a.r, keep, s_terms);
-  __syncthreads();
-  u32x4 pf[NSUB][RT];
+  auto weights = [&](int o, int j, int t) {  // o: the run's first column within the weights in LDS
+    if constexpr (TR) {
+      // The lane reads four columns of a rank; columns of a run are dealt 8 (row % 4) + 4 j.
+      const int r = 16 * t + 8 * (q & 1) + (row >> 2), x = o / 8 + (row & 3);
+      const char* p = reinterpret_cast<const char*>(s_w + r * CPR + ((((x >> 2) ^ (r & 3)) << 2) | (x & 3))) + 8 * j;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(p + 4 * CPR * 16));
+      u32x4 f;
+      __builtin_memcpy(&f, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&f) + 8, &hi, 8);
+      return f;
+    } else {
+      const int r = o + 8 * (row >> 2) + 4 * j + (row & 3);
+      return s_w[r * 2 * RT + ((2 * t + (q & 1)) ^ up_swizzle<RT>(r))];
+    }
+  };
+  u32x4 pf[RT];
+  auto load_terms = [&](int k0) {
 #pragma unroll
-  for (int s = 0; s < NSUB; ++s)
+    for (int t = 0; t < RT; ++t) {
+      if constexpr (TR) {
+        const int block = k0 / 16 + t;
+        pf[t] = block < a.blocksQ ? ld16(a.Qn + ((int64_t(ti) * kLoraTile + first + row) * a.blocksQ + block) * 32 + 8 * q)
+                                  : zero16();
+      } else {
+        pf[t] = ld16(s_terms + (first + row) * kUpPitch<RT> + t * 32 + 8 * q);
+      }
+    }
+  };
+  auto store = [&](int o, const u32x4& base, const f32x4 (&d)[2]) {
+    const float v[8] = {d[0][0], d[0][1], d[0][2], d[0][3], d[1][0], d[1][1], d[1][2], d[1][3]};
+    if (on && o + 8 * q < end) st16(yr + o, lora_add8(base, v));
+  };
+  if constexpr (MULTI) {
+    f32x4 d[UN][2];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) pf[s][t] = ld16(s_terms + (s * 16 + row) * kUpPitch<RT> + t * 32 + 8 * q);
-  while (o0 < end) {
+    for (int u = 0; u < UN; ++u) d[u][0] = d[u][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = 0; k0 < ranks; k0 += 16 * RT) {
+      stage_w(cb, k0);
+      load_terms(k0);
+      wait_vmcnt<0>();
+      block_sync();
 #pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int o = o0 + 128 * u + 8 * q;
+      for (int u = 0; u < UN; ++u)
+        if (u < per) {
 #pragma unroll
-      for (int s = 0; s < NSUB; ++s) {
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) d[u][j] = mfma16(weights(o0 - cb + stride * u, j, t), pf[t], d[u][j]);
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+      if (u < runs) store(o0 + stride * u, b[u], d[u]);
+  } else {
+    if constexpr (!TR) {
+      stage_w(cb, 0);
+      lora_stage<RT>(a, plan, tile, ti, 16 * subs, part * a.r, keep, s_terms);
+    } else {
+      stage_w(cb, 0);
+      load_terms(0);
+    }
+    wait_vmcnt<0>();
+    __syncthreads();
+    if constexpr (!TR) load_terms(0);
+    for (int i0 = 0; i0 < runs; i0 += UN) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const int i = i0 + u;
+        if (i >= runs) break;  // uniform, in the block too
+        if (i > 0 && i % per == 0) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          stage_w(cb + i / per * COLS, 0);
+          wait_vmcnt<0>();
+          block_sync();
+        }
         f32x4 d[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           d[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int t = 0; t < RT; ++t) d[j] = mfma16(wf[u][j][t], pf[s][t], d[j]);
+          for (int t = 0; t < RT; ++t) d[j] = mfma16(weights(o0 - cb + stride * (i % per), j, t), pf[t], d[j]);
         }
-        const float v[8] = {d[0][0], d[0][1], d[0][2], d[0][3], d[1][0], d[1][1], d[1][2], d[1][3]};
-        if (o < end && s * 16 + row < tile.count) st16(yr[s] + o, lora_add8(b[u][s], v));
+        store(o0 + stride * i, b[u], d);
+        load_base(i + UN, u);
       }
     }
-    o0 += 128 * UN;
-    if (o0 < end) load(o0);
   }
 }
 
-// Runs of 32 columns that a wave loads at once: up to 24 vectors of 16 bytes.
-template <int RT>
-constexpr int kUpRuns = RT == 1 ? 4 : RT <= 4 ? 2 : 1;
-
-template <int RT>
-__global__ __launch_bounds__(256) void lora_up_kernel(LoraUp a, LoraPlan plan) {
-  __shared__ __align__(16) uint16_t s_terms[64 * kUpPitch<RT>];
+template <int RT, bool TR, bool MULTI>
+__global__ __launch_bounds__(256, 2) void lora_up_kernel(LoraUp a, LoraPlan plan) {
+  __shared__ u32x4 s_w[kUpCols<RT> * 2 * RT];
+  __shared__ __align__(16) uint16_t s_terms[TR ? 8 : 64 * kUpPitch<RT>];
   const int blocks = a.first[a.parts], ti = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
-  int tok[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
   const LoraTile tile = plan.tile(plan.tiles, ti, 3);
   if (tile.count == 0) return;
   int part = 0;
@@ -601,90 +751,9 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraUp a, LoraPlan plan) {
   const bool keep = a.P != nullptr && cb == 0;
   if (tile.adapter >= plan.n)
     lora_copy(a, plan, tile, ti, a.off[part] + cb, min(a.span, a.width[part] - cb), part * a.r, keep ? a.r : 0);
-  else if (tile.count <= 16)
-    lora_up_body<RT, 1, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
-  else if (tile.count <= 32)
-    lora_up_body<RT, 2, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
   else
-    lora_up_body<RT, 4, kUpRuns<RT>>(a, plan, tile, ti, tok, part, cb, keep, s_terms);
-}
-
-constexpr int kUpTCols = 512;  // columns per block, 128 per wave
-
-// dX = base + Q A.  A's rows are ranks, so a lane loads eight ranks of eight
-// columns and transposes them in registers; eight instructions then give a
-// lane four runs of eight consecutive columns (32 apart) of one token.  Q's terms come as
-// lora_terms_kernel left them.
-template <int NSUB>
-__device__ __forceinline__ void lora_up_t_body(const LoraUp& a, const uint16_t* Qn, int blocksQ, int d_in,
-                                               const LoraTile& tile, int ti, const int (&tok)[4], int c0) {
-  const int lane = threadIdx.x & 63, row = lane & 15, q = lane >> 4;
-  const int wc = c0 + 8 * (4 * (row & 3) + (row >> 2));  // row 4 q + i of the products: columns 32 i + 8 q + c
-  const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + min(wc, d_in - 8);
-  const uint16_t* qn = Qn + (int64_t(ti) * kLoraTile + row) * blocksQ * 32 + 8 * q;
-  f32x4 acc[NSUB][8];
-#pragma unroll
-  for (int s = 0; s < NSUB; ++s)
-#pragma unroll
-    for (int c = 0; c < 8; ++c) acc[s][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  u32x4 v[8], b[2][4];
-  auto load_w = [&](int t) {
-    const int k = 16 * t + 8 * (q & 1);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = k < a.R ? ld16(w + int64_t(k + j) * d_in) : zero16();
-  };
-  auto load_base = [&](int s) {
-    const uint16_t* br = a.base + int64_t(tok[s]) * a.ld_base + c0 + 8 * q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) b[s & 1][i] = c0 + 32 * i + 8 * q < d_in ? ld16(br + 32 * i) : zero16();
-  };
-  load_w(0);
-  load_base(0);
-  if (NSUB > 1) load_base(1);
-  for (int t = 0; t < blocksQ; ++t) {
-    u32x4 wf[8], pf[NSUB];
-#pragma unroll
-    for (int s = 0; s < NSUB; ++s) pf[s] = ld16(qn + (int64_t(s) * 16 * blocksQ + t) * 32);
-    transpose8x8_b16(v, wf);
-    if (t + 1 < blocksQ) load_w(t + 1);
-#pragma unroll
-    for (int s = 0; s < NSUB; ++s)
-#pragma unroll
-      for (int c = 0; c < 8; ++c) acc[s][c] = mfma16(wf[c], pf[s], acc[s][c]);
-  }
-#pragma unroll
-  for (int s = 0; s < NSUB; ++s) {
-    uint16_t* yr = a.Y + int64_t(tok[s]) * a.ldy + c0 + 8 * q;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float d[8];
-#pragma unroll
-      for (int c = 0; c < 8; ++c) d[c] = acc[s][c][i];
-      if (c0 + 32 * i + 8 * q < d_in && s * 16 + row < tile.count) st16(yr + 32 * i, lora_add8(b[s & 1][i], d));
-    }
-    if (s + 2 < NSUB) load_base(s + 2);
-  }
-}
-
-__global__ __launch_bounds__(256) void lora_up_t_kernel(LoraUp a, const uint16_t* Qn, int blocksQ, int d_in,
-                                                        LoraPlan plan) {
-  const int blocks = (d_in + kUpTCols - 1) / kUpTCols, ti = blockIdx.x / blocks, cb = blockIdx.x % blocks * kUpTCols;
-  int tok[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) tok[s] = plan.tokens[ti * kLoraTile + 16 * s + (threadIdx.x & 15)];
-  const LoraTile tile = plan.tile(plan.tiles, ti, 3);
-  if (tile.count == 0) return;
-  const int c0 = cb + 128 * (threadIdx.x >> 6);
-  if (tile.adapter >= plan.n)
-    lora_copy(a, plan, tile, ti, cb, min(kUpTCols, d_in - cb), 0, 0);
-  else if (c0 >= d_in)
-    return;
-  else if (tile.count <= 16)
-    lora_up_t_body<1>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
-  else if (tile.count <= 32)
-    lora_up_t_body<2>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
-  else
-    lora_up_t_body<4>(a, Qn, blocksQ, d_in, tile, ti, tok, c0);
+    lora_up_body<RT, TR, MULTI>(a, plan, tile, ti, part, cb, keep, tile.count <= 16 ? 1 : tile.count <= 32 ? 2 : 4, s_w,
+                                s_terms);
 }
 
 // ---------------------------------------------------------------- products with the tokens contracted
@@ -708,11 +777,6 @@ struct LoraGrad {
 // Stages in LDS: two blocks per CU at 64 ranks (20 KiB a stage), three at 16 (11 KiB).
 template <int RT>
 constexpr int kGradStages = RT == 4 ? 3 : 4;
-
-// 16 bytes per lane from memory into LDS at lds + 16 lane (uniform), without a register between.
-__device__ __forceinline__ void lora_dma16(const void* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory");
-}
 
 // One block sums the products of up to 512 tokens of one adapter for 128
 // columns and 16 RT ranks.  A stage of the pipeline is 32 tokens: their rows
@@ -848,6 +912,28 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
 // Blocks of 16, 32 or 64 ranks.
 static int rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
 
+// Blocks of up to 1024 columns: the rank terms and the plan cost less per column, down to 128 where there are few tiles.
+template <bool TR>
+static hipError_t launch_up(LoraUp& u, int ranks, int tiles, const LoraPlan& plan, hipStream_t s) {
+  int cols = 0;
+  for (int p = 0; p < u.parts; ++p) cols += u.width[p];
+  u.span = 1024;
+  while (u.span > 128 && int64_t(tiles) * (cols / u.span) < 512) u.span /= 2;
+  if (ranks > 128) u.span = kUpCols<8>;
+  for (int p = 0, off = 0; p < u.parts; ++p) {
+    u.off[p] = off;
+    off += u.width[p];
+    u.first[p + 1] = u.first[p] + (u.width[p] + u.span - 1) / u.span;
+  }
+  const dim3 grid(unsigned(tiles) * unsigned(u.first[u.parts])), block(256);
+  if (ranks <= 16) hipLaunchKernelGGL((lora_up_kernel<1, TR, false>), grid, block, 0, s, u, plan);
+  else if (ranks <= 32) hipLaunchKernelGGL((lora_up_kernel<2, TR, false>), grid, block, 0, s, u, plan);
+  else if (ranks <= 64) hipLaunchKernelGGL((lora_up_kernel<4, TR, false>), grid, block, 0, s, u, plan);
+  else if (ranks <= 128) hipLaunchKernelGGL((lora_up_kernel<8, TR, false>), grid, block, 0, s, u, plan);
+  else if constexpr (TR) hipLaunchKernelGGL((lora_up_kernel<8, true, true>), grid, block, 0, s, u, plan);
+  return hipGetLastError();
+}
+
 static int round_slice(int K, int splits) {
   return ((K + splits - 1) / splits + kLoraSlice - 1) / kLoraSlice * kLoraSlice;
 }
@@ -868,21 +954,10 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   LoraUp u = {};
   u.part = part, u.splits = splits, u.R = R, u.scale = scale;
   u.W = B, u.wstride = int64_t(z.d_out) * z.r, u.r = z.r;
-  u.base = base, u.ld_base = ld_base, u.Y = Y, u.ldy = ldy, u.P = P, u.parts = z.parts;
-  // Blocks of 512 columns where that gives every CU a few; narrower ones below.
-  u.span = 512;
-  while (u.span > 128 && int64_t(tiles) * (z.d_out / u.span) < 1024) u.span /= 2;
-  for (int p = 0, off = 0; p < z.parts; ++p) {
-    u.off[p] = off, u.width[p] = z.widths[p];
-    off += z.widths[p];
-    u.first[p + 1] = u.first[p] + (z.widths[p] + u.span - 1) / u.span;
-  }
-  const dim3 grid(unsigned(tiles) * unsigned(u.first[z.parts])), block(256);
-  if (z.r <= 16) hipLaunchKernelGGL(lora_up_kernel<1>, grid, block, 0, s, u, pl);
-  else if (z.r <= 32) hipLaunchKernelGGL(lora_up_kernel<2>, grid, block, 0, s, u, pl);
-  else if (z.r <= 64) hipLaunchKernelGGL(lora_up_kernel<4>, grid, block, 0, s, u, pl);
-  else hipLaunchKernelGGL(lora_up_kernel<8>, grid, block, 0, s, u, pl);
-  return hipGetLastError();
+  u.base = base, u.ld_base = ld_base, u.Y = Y, u.ldy = ldy, u.P = P;
+  u.parts = z.parts;
+  for (int p = 0; p < z.parts; ++p) u.width[p] = z.widths[p];
+  return launch_up<false>(u, z.r, tiles, pl, s);
 }
 
 template <bool DB>
@@ -929,10 +1004,8 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
   if (dX) {
     LoraUp u = {};
     u.R = R, u.W = A, u.wstride = int64_t(R) * z.d_in, u.base = base, u.ld_base = ld_base, u.Y = dX, u.ldy = lddx;
-    const int blocks = (z.d_in + kUpTCols - 1) / kUpTCols;
-    hipLaunchKernelGGL(lora_up_t_kernel, dim3(unsigned(tiles) * unsigned(blocks)), dim3(256), 0, s, u, w.Qn, m.blocksQ,
-                       z.d_in, pl);
-    if ((e = hipGetLastError())) return e;
+    u.Qn = w.Qn, u.blocksQ = m.blocksQ, u.parts = 1, u.width[0] = z.d_in;
+    if ((e = launch_up<true>(u, R, tiles, pl, s))) return e;
   }
   LoraGrad g = {};
   if (dA) {
