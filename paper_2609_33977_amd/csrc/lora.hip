@@ -572,16 +572,9 @@ __device__ __forceinline__ void lora_copy(const LoraUp& a, const LoraPlan& plan,
     a.P[int64_t(tokens[e / ranks]) * a.R + rank0 + e % ranks] = 0.0f;
 }
 
-__device__ __forceinline__ u32x4 lora_add8(const u32x4& b, const float (&d)[8]) {
-  u32x4 r;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) r[p] = pack_bf16x2(bf16_lo(b[p]) + d[2 * p], bf16_hi(b[p]) + d[2 * p + 1]);
-  return r;
-}
-
-// Columns whose weights are in LDS at a time: 32 KiB of them, at most 512 columns.
+// Columns whose weights are in LDS at a time.
 template <int RT>
-constexpr int kUpCols = RT == 1 ? 512 : 1024 / RT;
+constexpr int kUpCols = RT <= 2 ? 512 : 256;
 
 // B's chunk of 8 ranks c of row o is at c ^ up_swizzle(o): the rows that eight lanes read at once then lie in
 // different 16-byte columns.
@@ -595,38 +588,67 @@ __device__ __forceinline__ int up_swizzle(int o) {
     return (o & 3) | ((o >> 3) & 1) << 2;
 }
 
+// Swaps a of the upper eight lanes of every 16 with b of the lower eight.
+__device__ __forceinline__ void lora_swap8(u32x4& a, u32x4& b, bool lower) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t give = lower ? b[i] : a[i];
+    const uint32_t got = uint32_t(__builtin_amdgcn_mov_dpp(int(give), 0x128, 0xf, 0xf, true));  // row_ror:8
+    a[i] = lower ? a[i] : got;
+    b[i] = lower ? got : b[i];
+  }
+}
+
 // Y = base + c P B^T, and with TR dX = base + Q A.  The matrix product's rows
 // are output columns and its columns tokens, with the columns dealt so that
-// two instructions leave eight consecutive ones of one token in each lane: base
-// and Y move as 16-byte vectors straight between memory and registers, 64 bytes
-// per token.  One instruction's 32 k hold the two terms of 16 ranks.
+// two instructions leave eight consecutive ones of one token in each lane.  One
+// instruction's 32 k hold the two terms of 16 ranks.  base and Y move between
+// memory and registers as 128 bytes of eight tokens at a time, 64 columns of 16
+// tokens per unit, and eight lanes of every 16 swap halves on the way: copying
+// 8192 rows of 11008 columns took 72 us so (5.0 TB/s) and 98 us as 64 bytes of 16 tokens, and not
+// keeping either in the caches pays at 128 bytes only (79 -> 75 us).
 //
 // A block takes 64 tokens and `span` columns; a wave 16 of the tokens and all
 // columns, or a share of the columns where there are fewer tokens.  The weights of kUpCols
 // columns at a time are copied into LDS, which all waves share; A's come back transposed.
-// base is loaded UN runs of 32 columns ahead.  More ranks than fit go in several rounds (MULTI),
-// with the sums of 128 columns held in registers.
+// base is loaded two units ahead.  More ranks than fit go in several rounds (MULTI),
+// with the sums of one round of columns held in registers.
 template <int RT, bool TR, bool MULTI>
 __device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& plan, const LoraTile& tile, int ti,
                                              int part, int cb, bool keep, int subs, u32x4* s_w, uint16_t* s_terms) {
-  constexpr int COLS = kUpCols<RT>, UN = 4, CPR = COLS / 8, COPIES = COLS * RT / 32;
-  static_assert(!MULTI || (TR && COLS == 32 * UN), "the sums of one round of columns stay in registers");
+  constexpr int COLS = kUpCols<RT>, UN = 2, CPR = COLS / 8, COPIES = COLS * RT / 32, UNIT = 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const int off = a.off[part], end = min(cb + a.span, a.width[part]), ranks = TR ? a.R : a.r;
-  const int share = 4 / subs, first = 16 * (wave % subs), o0 = cb + 32 * (wave / subs), stride = 32 * share;
-  const int runs = (end - cb + stride - 1) / stride, per = COLS / stride;  // of a wave: in all, and per weights in LDS
-  const int64_t tok = plan.tokens[ti * kLoraTile + first + row];
+  const int share = 4 / subs, first = 16 * (wave % subs), o0 = cb + UNIT * (wave / subs), stride = UNIT * share;
+  const int units = (end - cb + stride - 1) / stride, per = COLS / stride;  // of a wave: in all, and per weights in LDS
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride + int64_t(off) * (TR ? 1 : a.r);
-  uint16_t* yr = a.Y + tok * a.ldy + off + 8 * q;
-  const uint16_t* br = a.base + tok * a.ld_base + off;
-  const bool on = first + row < tile.count;
-  u32x4 b[UN];
+  // This lane's 16 bytes of a unit's two moves: tokens row % 8 and row % 8 + 8, columns 32 (row / 8) + 8 q.
+  const bool lower = row < 8;
+  const int mc = (lower ? 0 : 32) + 8 * q;
+  const uint16_t* br[2];
+  uint16_t* yr[2];
+  bool on[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = first + (row & 7) + 8 * h;
+    const int64_t tok = plan.tokens[ti * kLoraTile + i];
+    br[h] = a.base + tok * a.ld_base + off;
+    yr[h] = a.Y + tok * a.ldy + off;
+    on[h] = i < tile.count;
+  }
+  u32x4 b[UN][2];
   auto load_base = [&](int i, int u) {
     const int o = o0 + stride * i;
-    if (o < end) b[u] = ld16(br + min(o + 8 * q, end - 8));
-  };
+    if (o < end) {
 #pragma unroll
-  for (int u = 0; u < UN; ++u) load_base(u, u);
+      for (int h = 0; h < 2; ++h)
+        b[u][h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(br[h] + min(o + mc, end - 8)));
+    }
+  };
+  if constexpr (!MULTI) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) load_base(u, u);
+  }
   const uint32_t lds = lds_addr(s_w);
   // Weights of columns [c, c + COLS) and ranks [k0, k0 + 16 RT); none past the last column, whose products are
   // not stored; past the last rank others stand in, against zero terms.
@@ -676,61 +698,71 @@ __device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& pl
       }
     }
   };
-  auto store = [&](int o, const u32x4& base, const f32x4 (&d)[2]) {
-    const float v[8] = {d[0][0], d[0][1], d[0][2], d[0][3], d[1][0], d[1][1], d[1][2], d[1][3]};
-    if (on && o + 8 * q < end) st16(yr + o, lora_add8(base, v));
-  };
-  if constexpr (MULTI) {
-    f32x4 d[UN][2];
+  // d[g][j]: run g's columns 4 j .. + 3 of this lane's eight.
+  auto multiply = [&](int o, f32x4 (&d)[2][2]) {
 #pragma unroll
-    for (int u = 0; u < UN; ++u) d[u][0] = d[u][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) d[g][j] = mfma16(weights(o + 32 * g, j, t), pf[t], d[g][j]);
+  };
+  auto store = [&](int o, u32x4 (&v)[2], const f32x4 (&d)[2][2]) {
+    lora_swap8(v[0], v[1], lower);
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        v[g][p] = pack_bf16x2(bf16_lo(v[g][p]) + d[g][p >> 1][2 * (p & 1)], bf16_hi(v[g][p]) + d[g][p >> 1][2 * (p & 1) + 1]);
+    lora_swap8(v[0], v[1], lower);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (on[h] && o + mc < end) __builtin_nontemporal_store(v[h], reinterpret_cast<u32x4*>(yr[h] + o + mc));
+  };
+  const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+  if constexpr (MULTI) {
+    constexpr int MU = COLS / UNIT;
+    f32x4 d[MU][2][2];
+#pragma unroll
+    for (int u = 0; u < MU; ++u) d[u][0][0] = d[u][0][1] = d[u][1][0] = d[u][1][1] = zero;
     for (int k0 = 0; k0 < ranks; k0 += 16 * RT) {
       stage_w(cb, k0);
       load_terms(k0);
       wait_vmcnt<0>();
       block_sync();
 #pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (u < per) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int t = 0; t < RT; ++t) d[u][j] = mfma16(weights(o0 - cb + stride * u, j, t), pf[t], d[u][j]);
-        }
+      for (int u = 0; u < MU; ++u)
+        if (u < per) multiply(o0 - cb + stride * u, d[u]);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 #pragma unroll
-    for (int u = 0; u < UN; ++u)
-      if (u < runs) store(o0 + stride * u, b[u], d[u]);
+    for (int u = 0; u < MU; ++u)
+      if (u < units) {
+        load_base(u, 0);
+        store(o0 + stride * u, b[0], d[u]);
+      }
   } else {
-    if constexpr (!TR) {
-      stage_w(cb, 0);
+    stage_w(cb, 0);
+    if constexpr (!TR)
       lora_stage<RT>(a, plan, tile, ti, 16 * subs, part * a.r, keep, s_terms);
-    } else {
-      stage_w(cb, 0);
+    else
       load_terms(0);
-    }
     wait_vmcnt<0>();
     __syncthreads();
     if constexpr (!TR) load_terms(0);
-    for (int i0 = 0; i0 < runs; i0 += UN) {
+    for (int i0 = 0; i0 < units; i0 += UN) {
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
         const int i = i0 + u;
-        if (i >= runs) break;  // uniform, in the block too
+        if (i >= units) break;  // uniform, in the block too
         if (i > 0 && i % per == 0) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           stage_w(cb + i / per * COLS, 0);
           wait_vmcnt<0>();
           block_sync();
         }
-        f32x4 d[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          d[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int t = 0; t < RT; ++t) d[j] = mfma16(weights(o0 - cb + stride * (i % per), j, t), pf[t], d[j]);
-        }
+        f32x4 d[2][2] = {{zero, zero}, {zero, zero}};
+        multiply(o0 - cb + stride * (i % per), d);
         store(o0 + stride * i, b[u], d);
         load_base(i + UN, u);
       }
@@ -739,7 +771,7 @@ __device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& pl
 }
 
 template <int RT, bool TR, bool MULTI>
-__global__ __launch_bounds__(256, 2) void lora_up_kernel(LoraUp a, LoraPlan plan) {
+__global__ __launch_bounds__(256, RT == 8 && !TR ? 1 : 2) void lora_up_kernel(LoraUp a, LoraPlan plan) {
   __shared__ u32x4 s_w[kUpCols<RT> * 2 * RT];
   __shared__ __align__(16) uint16_t s_terms[TR ? 8 : 64 * kUpPitch<RT>];
   const int blocks = a.first[a.parts], ti = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
@@ -912,13 +944,13 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
 // Blocks of 16, 32 or 64 ranks.
 static int rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
 
-// Blocks of up to 1024 columns: the rank terms and the plan cost less per column, down to 128 where there are few tiles.
+// Blocks of up to 1024 columns: the rank terms and the plan cost less per column, down to 256 where there are few tiles.
 template <bool TR>
 static hipError_t launch_up(LoraUp& u, int ranks, int tiles, const LoraPlan& plan, hipStream_t s) {
   int cols = 0;
   for (int p = 0; p < u.parts; ++p) cols += u.width[p];
   u.span = 1024;
-  while (u.span > 128 && int64_t(tiles) * (cols / u.span) < 512) u.span /= 2;
+  while (u.span > 256 && int64_t(tiles) * (cols / u.span) < 512) u.span /= 2;
   if (ranks > 128) u.span = kUpCols<8>;
   for (int p = 0, off = 0; p < u.parts; ++p) {
     u.off[p] = off;
