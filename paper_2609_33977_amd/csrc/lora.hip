@@ -198,7 +198,7 @@ struct LoraDown {
   int K, wrows;
   float* part;  // [splits][T][R], rows in the plan's order
   int R;
-  int splits, slice;  // K per split, a multiple of kLoraSlice
+  int splits;
   int off[kLoraMaxParts], width[kLoraMaxParts];  // B: the parts' columns
   int chunks;                                    // blocks of 16 RT ranks per part
 };
@@ -221,18 +221,19 @@ __device__ __forceinline__ u32x4 lora_tr_frag(const char* base, int pitch, int c
   return f;
 }
 
-constexpr int kDownK = 64;  // contraction length per stage
+constexpr int kDownK = 64;     // contraction length per stage
+constexpr int kDownUnit = 128;  // dealt to the splits in turn: blocks that run together read neighbouring k
 // 16-byte slots of LDS: four stages of 64 tokens and 16 RT ranks.
 template <int RT>
 constexpr int kDownSlots = 4 * (8 + 2 * RT) * 64;
 
-// part[s][p][c] = sum over split s's K range of X[token p][k] W[c][k], for a
+// part[s][p][c] = sum over split s's share of K of X[token p][k] W[c][k], for a
 // tile of 17 to 64 tokens: 64 k of the tokens' rows and of the adapter are copied into LDS three stages ahead;
 // each wave takes 16 tokens and all ranks.  B is contracted over its rows,
 // which come back transposed.
 template <int RT, bool BMAJOR>
-__device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile& tile, const int* tokens, int k0,
-                                               int k1, int col0, int r0, int nr, float* out, u32x4* s_mem) {
+__device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile& tile, const int* tokens,
+                                               int split, int K, int col0, int r0, int nr, float* out, u32x4* s_mem) {
   constexpr int NS = 4, COPIES = 8 + 2 * RT, PER = (COPIES + 3) / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const uint32_t lds = lds_addr(s_mem);
@@ -259,20 +260,22 @@ __device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile
       src[i] = reinterpret_cast<const char*>(w + int64_t(col0) * a.wrows + r0 + min(8 * (e % (2 * RT)), nr - 8));
     }
   }
-  // Past the range's end the last values stand in, against zeros of the adapter.
+  auto first_k = [&](int step) { return ((step >> 1) * a.splits + split) * kDownUnit + (step & 1) * kDownK; };
+  // Past K the last values stand in, against zeros of the adapter.
   auto issue = [&](int step) {
     const uint32_t at = lds + uint32_t(step % NS) * (COPIES * 1024);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = min(wave + 4 * i, COPIES - 1), k = k0 + step * kDownK + kl[i];
-      const char* p = BMAJOR && c >= 8 ? src[i] + int64_t(min(k, k1 - 1)) * a.wrows * 2 : src[i] + int64_t(min(k, k1 - 8)) * 2;
+      const int c = min(wave + 4 * i, COPIES - 1), k = first_k(step) + kl[i];
+      const char* p = BMAJOR && c >= 8 ? src[i] + int64_t(min(k, K - 1)) * a.wrows * 2 : src[i] + int64_t(min(k, K - 8)) * 2;
       lora_dma16(p, __builtin_amdgcn_readfirstlane(at + uint32_t(c) * 1024));
     }
   };
   f32x4 acc[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int steps = (k1 - k0 + kDownK - 1) / kDownK;
+  const int units = ((K + kDownUnit - 1) / kDownUnit - split + a.splits - 1) / a.splits;  // at least one
+  const int steps = 2 * units - (first_k(2 * units - 1) >= K ? 1 : 0);
   for (int s = 0; s < NS - 1 && s < steps; ++s) issue(s);
   for (int s = 0; s < steps; ++s) {
     wait_stages<PER>(min(steps - 1 - s, NS - 2));
@@ -283,7 +286,7 @@ __device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 x = km_frag(st + h * 256, 16 * wave, lane);
-      const bool in = k0 + s * kDownK + 32 * h + 8 * q < k1;
+      const bool in = first_k(s) + 32 * h + 8 * q < K;
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
         u32x4 f = BMAJOR ? lora_tr_frag(reinterpret_cast<const char*>(st + 512) + 32 * h * (32 * RT), 32 * RT, 16 * t, lane)
@@ -306,35 +309,36 @@ __device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile
 // counts: the waves take 128 of every 512 k and add up through LDS, and
 // fragments come straight from memory into registers, four steps of 32 k ahead.
 template <int RT, bool BMAJOR>
-__device__ __forceinline__ void lora_down_few(const LoraDown& a, const LoraTile& tile, int tok, int k0, int k1, int col0,
-                                              int r0, int nr, float* out, u32x4* s_mem) {
+__device__ __forceinline__ void lora_down_few(const LoraDown& a, const LoraTile& tile, int tok, int split, int K,
+                                              int col0, int r0, int nr, float* out, u32x4* s_mem) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const uint16_t* xr = a.X + int64_t(tok) * a.ldx + col0;
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride;
+  const int k0 = split * kLoraSlice, next = a.splits * kLoraSlice;
   f32x4 acc[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   u32x4 x[4];
-  auto load_x = [&](int kw, int j) { x[j] = ld16(xr + min(kw + 32 * j + 8 * q, k1 - 8)); };
+  auto load_x = [&](int kw, int j) { x[j] = ld16(xr + min(kw + 32 * j + 8 * q, K - 8)); };
   if constexpr (!BMAJOR) {
     u32x4 wf[RT][4];
     const uint16_t* wr[RT];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) wr[t] = w + int64_t(r0 + min(t * 16 + row, nr - 1)) * a.K;
+    for (int t = 0; t < RT; ++t) wr[t] = w + int64_t(r0 + min(t * 16 + row, nr - 1)) * K;
     auto load_w = [&](int kw, int j) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) wf[t][j] = ld16(wr[t] + min(kw + 32 * j + 8 * q, k1 - 8));
+      for (int t = 0; t < RT; ++t) wf[t][j] = ld16(wr[t] + min(kw + 32 * j + 8 * q, K - 8));
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
-    for (int kb = k0; kb < k1; kb += kLoraSlice) {
+    for (int kb = k0; kb < K; kb += next) {
       const int kw = kb + wave * 128;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool in = kw + 32 * j + 8 * q < k1;
+        const bool in = kw + 32 * j + 8 * q < K;
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[t] = mfma16(x[j], in ? wf[t][j] : zero16(), acc[t]);
-        if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
+        if (kb + next < K) load_x(kw + next, j), load_w(kw + next, j);
       }
     }
   } else {
@@ -346,12 +350,12 @@ __device__ __forceinline__ void lora_down_few(const LoraDown& a, const LoraTile&
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         const int e = i * 64 + lane;
-        v[i][j] = ld16(w + int64_t(min(kw + 32 * j + e / CH, k1 - 1)) * a.wrows + min(8 * (e % CH), nr - 8));
+        v[i][j] = ld16(w + int64_t(min(kw + 32 * j + e / CH, K - 1)) * a.wrows + min(8 * (e % CH), nr - 8));
       }
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) load_x(k0 + wave * 128, j), load_w(k0 + wave * 128, j);
-    for (int kb = k0; kb < k1; kb += kLoraSlice) {
+    for (int kb = k0; kb < K; kb += next) {
       const int kw = kb + wave * 128;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -359,13 +363,13 @@ __device__ __forceinline__ void lora_down_few(const LoraDown& a, const LoraTile&
 #pragma unroll
         for (int i = 0; i < RT; ++i) sw[i * 64 + lane] = v[i][j];
         __syncthreads();
-        const bool in = kw + 32 * j + 8 * q < k1;
+        const bool in = kw + 32 * j + 8 * q < K;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
           const u32x4 f = lora_tr_frag(reinterpret_cast<const char*>(sw), 32 * RT, 16 * t, lane);
           acc[t] = mfma16(x[j], in ? f : zero16(), acc[t]);
         }
-        if (kb + kLoraSlice < k1) load_x(kw + kLoraSlice, j), load_w(kw + kLoraSlice, j);
+        if (kb + next < K) load_x(kw + next, j), load_w(kw + next, j);
       }
     }
   }
@@ -395,14 +399,13 @@ __global__ __launch_bounds__(256, 2) void lora_down_kernel(LoraDown a, LoraPlan 
   const int chunk = blockIdx.y % a.chunks, part = BMAJOR ? blockIdx.y / a.chunks : 0;
   const int r0 = chunk * 16 * RT, nr = min(16 * RT, a.wrows - r0);
   const int col0 = BMAJOR ? a.off[part] : 0, K = BMAJOR ? a.width[part] : a.K;
-  const int k0 = split * a.slice, k1 = min(k0 + a.slice, K);
   float* out = a.part + (int64_t(split) * plan.T + tile.pos) * a.R + part * a.wrows + r0;
-  if (k0 >= k1) {  // a narrower part than the widest
+  if (split * kLoraSlice >= K) {  // a narrower part than the widest has no slice for this split
     for (int e = threadIdx.x; e < tile.count * nr; e += 256) out[int64_t(e / nr) * a.R + e % nr] = 0.0f;
   } else if (tile.count <= 16) {
-    lora_down_few<RT, BMAJOR>(a, tile, tok, k0, k1, col0, r0, nr, out, s_mem);
+    lora_down_few<RT, BMAJOR>(a, tile, tok, split, K, col0, r0, nr, out, s_mem);
   } else {
-    lora_down_wide<RT, BMAJOR>(a, tile, tokens, k0, k1, col0, r0, nr, out, s_mem);
+    lora_down_wide<RT, BMAJOR>(a, tile, tokens, split, K, col0, r0, nr, out, s_mem);
   }
 }
 
@@ -966,10 +969,6 @@ static hipError_t launch_up(LoraUp& u, int ranks, int tiles, const LoraPlan& pla
   return hipGetLastError();
 }
 
-static int round_slice(int K, int splits) {
-  return ((K + splits - 1) / splits + kLoraSlice - 1) / kLoraSlice * kLoraSlice;
-}
-
 hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, const float* scale,
                            const void* plan, const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* Y,
                            int64_t ldy, float* P, float* part, int splits, hipStream_t s) {
@@ -978,7 +977,6 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   LoraDown d = {};
   d.X = X, d.ldx = ldx, d.W = A, d.wstride = int64_t(R) * z.d_in, d.K = z.d_in, d.wrows = R;
   d.part = part, d.R = R;
-  d.slice = round_slice(z.d_in, splits);
   d.splits = splits;
   const int rt = rank_tiles(R);
   d.chunks = (R + 16 * rt - 1) / (16 * rt);
@@ -1021,7 +1019,7 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
   if (dX || dA) {
     LoraDown d = {};
     d.X = dY, d.ldx = lddy, d.W = B, d.wstride = int64_t(z.d_out) * z.r, d.K = widest, d.wrows = z.r;
-    d.part = w.part, d.R = R, d.splits = splits, d.slice = round_slice(widest, splits);
+    d.part = w.part, d.R = R, d.splits = splits;
     for (int p = 0; p < z.parts; ++p) d.off[p] = off[p], d.width[p] = z.widths[p];
     const int rt = rank_tiles(z.r);
     d.chunks = (z.r + 16 * rt - 1) / (16 * rt);
