@@ -221,78 +221,76 @@ __device__ __forceinline__ u32x4 lora_tr_frag(const char* base, int pitch, int c
   return f;
 }
 
-constexpr int kDownK = 64;     // contraction length per stage
-constexpr int kDownUnit = 128;  // dealt to the splits in turn: blocks that run together read neighbouring k
-// 16-byte slots of LDS: four stages of 64 tokens and 16 RT ranks.
+constexpr int kDownK = 128;  // contraction length per stage, dealt to the splits in turn
+
+// Stages in LDS, each 16 KiB of tokens and 4 RT KiB of the adapter: two blocks per CU, three at 16 ranks.  With two
+// stages of 128 k 8192 tokens of 11008 columns and 64 ranks took 44 us, with four of 64 k 47.
 template <int RT>
-constexpr int kDownSlots = 4 * (8 + 2 * RT) * 64;
+constexpr int kDownStages = RT == 4 ? 2 : 3;
+template <int RT>
+constexpr int kDownSlots = kDownStages<RT> * (16 + 4 * RT) * 64;  // of 16 bytes
 
 // part[s][p][c] = sum over split s's share of K of X[token p][k] W[c][k], for a
-// tile of 17 to 64 tokens: 64 k of the tokens' rows and of the adapter are copied into LDS three stages ahead;
-// each wave takes 16 tokens and all ranks.  B is contracted over its rows,
-// which come back transposed.
+// tile of 17 to 64 tokens: 128 k of the tokens' rows and of the adapter are copied into LDS ahead of their use;
+// each wave takes 16 tokens and all ranks.  Splits take every splits-th 128 k, so that
+// blocks that run together read neighbouring columns.  B is contracted over its
+// rows, which come back transposed.
 template <int RT, bool BMAJOR>
 __device__ __forceinline__ void lora_down_wide(const LoraDown& a, const LoraTile& tile, const int* tokens,
                                                int split, int K, int col0, int r0, int nr, float* out, u32x4* s_mem) {
-  constexpr int NS = 4, COPIES = 8 + 2 * RT, PER = (COPIES + 3) / 4;
+  constexpr int NS = kDownStages<RT>, COPIES = 16 + 4 * RT, PER = COPIES / 4;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const uint32_t lds = lds_addr(s_mem);
   const uint16_t* w = a.W + int64_t(tile.adapter) * a.wstride;
-  // Copy c < 8: 32 k (half c / 4) of 16 tokens; then the adapter's ranks of both halves, or rows of B.
-  const char* src[PER];
-  int kl[PER];  // k within the stage of this lane's 16 bytes
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int c = min(wave + 4 * i, COPIES - 1);  // a wave with fewer repeats the last
-    int r, chunk;
-    if (c < 8) {
-      km_dma_target((c & 3) * 64 + lane, r, chunk);
-      kl[i] = 32 * (c >> 2) + 8 * chunk;
-      src[i] = reinterpret_cast<const char*>(a.X + int64_t(tokens[r]) * a.ldx + col0);
-    } else if (!BMAJOR) {
-      const int f = c - 8;
-      km_dma_target((f % RT) * 64 + lane, r, chunk);
-      kl[i] = 32 * (f / RT) + 8 * chunk;
-      src[i] = reinterpret_cast<const char*>(w + int64_t(r0 + min(r, nr - 1)) * a.K);
-    } else {
-      const int e = (c - 8) * 64 + lane;
-      kl[i] = e / (2 * RT);
-      src[i] = reinterpret_cast<const char*>(w + int64_t(col0) * a.wrows + r0 + min(8 * (e % (2 * RT)), nr - 8));
-    }
-  }
-  auto first_k = [&](int step) { return ((step >> 1) * a.splits + split) * kDownUnit + (step & 1) * kDownK; };
-  // Past K the last values stand in, against zeros of the adapter.
+  // Copy c < 16: 32 k (quarter c / 4) of 16 tokens, the wave's own; then 32 k of 16 ranks, or 1 KiB of B's rows.
+  int tr, tchunk;
+  km_dma_target(wave * 64 + lane, tr, tchunk);
+  const uint16_t* x = a.X + int64_t(tokens[tr]) * a.ldx + col0;
   auto issue = [&](int step) {
     const uint32_t at = lds + uint32_t(step % NS) * (COPIES * 1024);
+    const int k0 = (step * a.splits + split) * kDownK;
+    // Past K the last values stand in, against zeros of the adapter.
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int c = min(wave + 4 * i, COPIES - 1), k = first_k(step) + kl[i];
-      const char* p = BMAJOR && c >= 8 ? src[i] + int64_t(min(k, K - 1)) * a.wrows * 2 : src[i] + int64_t(min(k, K - 8)) * 2;
-      lora_dma16(p, __builtin_amdgcn_readfirstlane(at + uint32_t(c) * 1024));
+    for (int i = 0; i < 4; ++i)
+      lora_dma16(x + min(k0 + 32 * i + 8 * tchunk, K - 8),
+                 __builtin_amdgcn_readfirstlane(at + uint32_t(wave + 4 * i) * 1024));
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int f = wave + 4 * i;
+      const uint16_t* p;
+      if constexpr (BMAJOR) {
+        const int e = f * 64 + lane;
+        p = w + int64_t(col0 + min(k0 + e / (2 * RT), K - 1)) * a.wrows + r0 + min(8 * (e % (2 * RT)), nr - 8);
+      } else {
+        int r, chunk;
+        km_dma_target((f % RT) * 64 + lane, r, chunk);
+        p = w + int64_t(r0 + min(r, nr - 1)) * K + min(k0 + 32 * (f / RT) + 8 * chunk, K - 8);
+      }
+      lora_dma16(p, __builtin_amdgcn_readfirstlane(at + uint32_t(16 + f) * 1024));
     }
   };
   f32x4 acc[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int units = ((K + kDownUnit - 1) / kDownUnit - split + a.splits - 1) / a.splits;  // at least one
-  const int steps = 2 * units - (first_k(2 * units - 1) >= K ? 1 : 0);
+  const int steps = ((K + kDownK - 1) / kDownK - split + a.splits - 1) / a.splits;  // at least one
   for (int s = 0; s < NS - 1 && s < steps; ++s) issue(s);
   for (int s = 0; s < steps; ++s) {
+    // stage s has landed, and the stage that is filled next has been read by every wave
     wait_stages<PER>(min(steps - 1 - s, NS - 2));
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     block_sync();
     if (s + NS - 1 < steps) issue(s + NS - 1);
     const u32x4* st = s_mem + s % NS * (COPIES * 64);
+    const int left = K - (s * a.splits + split) * kDownK;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const u32x4 x = km_frag(st + h * 256, 16 * wave, lane);
-      const bool in = first_k(s) + 32 * h + 8 * q < K;
+    for (int h = 0; h < 4; ++h) {
+      const u32x4 xf = km_frag(st + h * 256, 16 * wave, lane);
 #pragma unroll
       for (int t = 0; t < RT; ++t) {
-        u32x4 f = BMAJOR ? lora_tr_frag(reinterpret_cast<const char*>(st + 512) + 32 * h * (32 * RT), 32 * RT, 16 * t, lane)
-                         : km_frag(st + 512 + h * 64 * RT, 16 * t, lane);
-        f = in ? f : zero16();
-        acc[t] = mfma16(x, f, acc[t]);
+        u32x4 f = BMAJOR ? lora_tr_frag(reinterpret_cast<const char*>(st + 1024) + 32 * h * (32 * RT), 32 * RT, 16 * t, lane)
+                         : km_frag(st + 1024 + h * 64 * RT, 16 * t, lane);
+        if (left < kDownK) f = 32 * h + 8 * q < left ? f : zero16();
+        acc[t] = mfma16(xf, f, acc[t]);
       }
     }
   }
