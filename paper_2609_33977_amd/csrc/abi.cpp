@@ -323,7 +323,7 @@ struct LoraBwdLayout {
 LoraBwdLayout lora_bwd_layout(const gm::LoraShape& z) {
   LoraBwdLayout Y;
   const size_t low = size_t(z.T) * z.parts * z.r * sizeof(float);
-  const size_t g = size_t(gm::lora_plan_layout(z.T, z.n).max_gtiles);
+  const size_t g = size_t(gm::lora_plan_layout(z.T, z.n).max_gtiles[gm::lora_bwd_glen(z)]);
   size_t off = 0;
   auto take = [&](size_t& at, size_t bytes) {
     at = off;

@@ -101,6 +101,7 @@ struct LoraBwdWs {
   float* partA;  // [gradient tiles][parts r][d_in]
   float* partB;  // [gradient tiles][d_out][r]
 };
+int lora_bwd_glen(const LoraShape& z);  // which of the plan's lengths the gradients take
 hipError_t launch_lora_plan(const int* adapter, int T, int n, void* plan, hipStream_t s);
 hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, const float* scale,
                            const void* plan, const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* Y,

@@ -13,9 +13,11 @@ constexpr int kLoraSlice = 512;     // contraction length that a block takes at 
 constexpr int kLoraGradCols = 128;  // columns of a gradient tile
 constexpr int32_t kLoraMagic = 0x61d7a3c5;
 
-// Tokens of one adapter whose gradient products one block sums up: longer runs
-// cost fewer partial sums, shorter ones fill the chip.
-inline int lora_grad_tokens(int64_t T) { return T > 4096 ? 512 : 256; }
+// Tokens of one adapter whose gradient products one block sums up: the plan
+// holds a table for each of these lengths.
+constexpr int kLoraGradLens = 4;
+constexpr int kLoraGradTokens = 256;  // the shortest; each is twice the last
+constexpr int kLoraGradMost = kLoraGradTokens << (kLoraGradLens - 1);
 
 // Most tiles of `tile` tokens that T tokens in m buckets can need.
 inline int64_t lora_tiles(int64_t T, int64_t buckets, int64_t tile) {
@@ -23,31 +25,43 @@ inline int64_t lora_tiles(int64_t T, int64_t buckets, int64_t tile) {
   return (T + (tile - 1) * m) / tile;
 }
 
-// The plan, in 4-byte words: a header (magic, T, n, tiles, gradient tiles);
-// the tile table, tokens of one adapter at a time, those without one last
-// (first position in that order, tokens, adapter, 0); 64 tokens for every tile
-// (the last one repeated); the gradient tile table (first tile, tokens,
-// adapter, only tile of its adapter); and each adapter's first gradient tile.
+// The plan, in 4-byte words: a header (magic, T, n, tiles, gradient tiles of
+// each length); the tile table, tokens of one adapter at a time, those without
+// one last (first position in that order, tokens, adapter, 0); 64 tokens for
+// every tile (the last one repeated); for each length the gradient tile table (first
+// tile, tokens, adapter, only tile of its adapter) and each adapter's first entry in it.
 struct LoraPlanLayout {
-  size_t tiles, tokens, gtiles, gstart, words;
-  int64_t max_tiles, max_gtiles;
+  size_t tiles, tokens, gtiles[kLoraGradLens], gstart[kLoraGradLens], words;
+  int64_t max_tiles, max_gtiles[kLoraGradLens];
 };
 
 inline LoraPlanLayout lora_plan_layout(int64_t T, int64_t n) {
   LoraPlanLayout L;
-  L.max_tiles = lora_tiles(T, n + 1, kLoraTile);
-  L.max_gtiles = lora_tiles(T, n, lora_grad_tokens(T));
   size_t at = 16;
   auto take = [&](size_t& w, size_t words) {
     w = at;
     at = (at + words + 15) / 16 * 16;
   };
+  L.max_tiles = lora_tiles(T, n + 1, kLoraTile);
   take(L.tiles, size_t(L.max_tiles) * 4);
   take(L.tokens, size_t(L.max_tiles) * kLoraTile);
-  take(L.gtiles, size_t(L.max_gtiles) * 4);
-  take(L.gstart, size_t(n) + 1);
+  for (int i = 0; i < kLoraGradLens; ++i) {
+    L.max_gtiles[i] = lora_tiles(T, n, kLoraGradTokens << i);
+    take(L.gtiles[i], size_t(L.max_gtiles[i]) * 4);
+    take(L.gstart[i], size_t(n) + 1);
+  }
   L.words = at;
   return L;
+}
+
+// Which length the gradients of T tokens take: the longest with enough blocks
+// of 128 columns (`col_blocks` for all tokens once) to fill the chip, since every
+// tile of an adapter beyond the first leaves partial sums to be written and added.
+constexpr int kLoraGradBlocks = 400;
+inline int lora_grad_len(int64_t T, int64_t col_blocks) {
+  int i = kLoraGradLens - 1;
+  while (i > 0 && (T + (kLoraGradTokens << i) - 1) / (kLoraGradTokens << i) * col_blocks < kLoraGradBlocks) --i;
+  return i;
 }
 
 // Blocks that share a tile's contraction over K: enough to fill the chip with

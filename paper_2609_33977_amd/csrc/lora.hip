@@ -42,10 +42,10 @@ struct LoraPlan {
   const int* head;
   const LoraTile* tiles;
   const int* tokens;
-  const LoraTile* gtiles;
+  const LoraTile* gtiles;  // of the length in use
   const int* gstart;
-  int T, n;
-  // Tile i of the table, without tokens if there is none: past the last, or in a
+  int glen, T, n;
+  // Entry i of a table with head[which] of them, without tokens if there is none: past the last, or in a
   // plan that was made for other sizes.  Header, entry and the tile's tokens do not wait for one another.
   __device__ __forceinline__ LoraTile tile(const LoraTile* table, int i, int which) const {
     const int magic = head[0], hT = head[1], hn = head[2], count = head[which];
@@ -55,11 +55,11 @@ struct LoraPlan {
   }
 };
 
-static LoraPlan lora_plan(const void* plan, int T, int n) {
+static LoraPlan lora_plan(const void* plan, int T, int n, int glen) {
   const LoraPlanLayout L = lora_plan_layout(T, n);
   const int* w = static_cast<const int*>(plan);
   return {w, reinterpret_cast<const LoraTile*>(w + L.tiles), w + L.tokens,
-          reinterpret_cast<const LoraTile*>(w + L.gtiles), w + L.gstart, T, n};
+          reinterpret_cast<const LoraTile*>(w + L.gtiles[glen]), w + L.gstart[glen], glen, T, n};
 }
 
 // Lanes of the wave with the same key, as a mask.
@@ -72,119 +72,145 @@ __device__ __forceinline__ uint64_t same_key(int key, int bits, bool on) {
   return m;
 }
 
-constexpr int kPlanMaxWaves = 16, kPlanBatch = 8;
+constexpr int kPlanBatch = 8;  // runs of 64 ids that a wave loads at once
+
+struct LoraPlanOut {
+  int* head;
+  LoraTile* tiles;
+  int* tokens;
+  LoraTile* gtiles[kLoraGradLens];
+  int* gstart[kLoraGradLens];
+};
+
+// Per bucket, scanned together: its first position and tile and its first gradient tile of each length, 14 bits or more each.
+struct LoraFirst {
+  uint64_t a;  // position, 20 bits | tile << 20 | gradient tiles << 34 and << 48
+  uint32_t b;  // gradient tiles, 16 bits each
+  __device__ __forceinline__ int pos() const { return int(a & 0xfffff); }
+  __device__ __forceinline__ int tile() const { return int(a >> 20) & 0x3fff; }
+  __device__ __forceinline__ int gtile(int i) const {
+    return i == 0 ? int(a >> 34) & 0x3fff : i == 1 ? int(a >> 48) : i == 2 ? int(b & 0xffff) : int(b >> 16);
+  }
+  __device__ __forceinline__ void add(const LoraFirst& o) { a += o.a, b += o.b; }
+};
+static_assert(kLoraGradLens == 4, "fields of LoraFirst");
 
 // A stable counting sort of the tokens by adapter in one block: each wave
 // counts and later places a contiguous run of tokens, so that equal adapters
-// keep their tokens' order and sums over them do not depend on timing.  No
-// atomics: the lanes of one key elect a leader.  One launch per batch serves
-// every linear of the model.  Bound by latency: the ids of 512 tokens are loaded at a time.
-__global__ __launch_bounds__(64 * kPlanMaxWaves) void lora_plan_kernel(const int* __restrict__ adapter, int T, int n,
-                                                                       int gtokens, int* __restrict__ head,
-                                                                       LoraTile* __restrict__ tiles,
-                                                                       int* __restrict__ tokens,
-                                                                       LoraTile* __restrict__ gtiles,
-                                                                       int* __restrict__ gstart) {
-  extern __shared__ int s_count[];  // [waves][n + 1], then the buckets' first positions, tiles and gradient tiles [n + 2]
-  __shared__ int s_sum[3][kPlanMaxWaves];
-  const int nb = n + 1, tid = threadIdx.x, NT = blockDim.x, waves = NT >> 6, lane = tid & 63, wave = tid >> 6;
-  int* s_start = s_count + waves * nb;
-  int* s_tile = s_start + nb + 1;
-  int* s_gtile = s_tile + nb + 1;
-  for (int i = tid; i < waves * nb; i += NT) s_count[i] = 0;
-  __syncthreads();
+// keep their tokens' order and sums over them do not depend on timing: the lanes
+// of one key elect a leader, which adds to its wave's own counter in LDS (an
+// atomic only so that the wave need not wait for it; a wave's LDS operations run in
+// order).  One launch per batch serves every linear of the model.  Bound by
+// latency, of instructions too: they run once, so loops stay rolled (10 KB of
+// code took 13 us for 8192 tokens).  The ids of 512 tokens per wave are loaded at a time.
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void lora_plan_kernel(const int* __restrict__ adapter, int T, int n,
+                                                              LoraPlanOut out) {
+  extern __shared__ int s_count[];  // [WAVES][n + 1], then the buckets' first entries [n + 2] and last tokens [n + 1]
+  __shared__ LoraFirst s_sum[WAVES];
+  __shared__ int s_ids[WAVES][64 * kPlanBatch];
+  constexpr int NT = 64 * WAVES;
+  const int nb = n + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  LoraFirst* s_first = reinterpret_cast<LoraFirst*>(s_count + (WAVES * nb + 1) / 2 * 2);
+  int* s_last = reinterpret_cast<int*>(s_first + nb + 1);
   const int bits = 32 - __builtin_clz(n);
   const int per = (T + NT - 1) / NT * 64;  // tokens per wave
   const int t0 = min(wave * per, T), t1 = min(t0 + per, T);
   int* mine = s_count + wave * nb;
-  int ids[kPlanBatch];
   auto load_ids = [&](int t) {
+    int ids[kPlanBatch];
 #pragma unroll
-    for (int i = 0; i < kPlanBatch; ++i) {
-      const int a = t + 64 * i + lane < t1 ? adapter[t + 64 * i + lane] : n;
-      ids[i] = unsigned(a) < unsigned(n) ? a : n;
-    }
+    for (int i = 0; i < kPlanBatch; ++i) ids[i] = adapter[min(t + 64 * i + lane, T - 1)];
+#pragma unroll
+    for (int i = 0; i < kPlanBatch; ++i) s_ids[wave][64 * i + lane] = unsigned(ids[i]) < unsigned(n) ? ids[i] : n;
   };
-  for (int t = t0; t < t1; t += 64 * kPlanBatch) {
-    load_ids(t);
-#pragma unroll
-    for (int i = 0; i < kPlanBatch; ++i) {
-      if (t + 64 * i >= t1) break;  // uniform
-      const bool on = t + 64 * i + lane < t1;
-      const uint64_t m = same_key(ids[i], bits, on);
-      if (on && (m & ((uint64_t(1) << lane) - 1)) == 0) mine[ids[i]] += __popcll(m);
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
+  for (int i = tid; i < WAVES * nb; i += NT) s_count[i] = 0;
   __syncthreads();
-  // Totals of a run of buckets per thread, scanned over the block; a wave's
-  // counts become its first position within the bucket.
-  const int run = (nb + NT - 1) / NT, b0 = min(tid * run, nb), b1 = min(b0 + run, nb);
-  int c[3] = {0, 0, 0};
-  for (int b = b0; b < b1; ++b) {
-    int tot = 0;
-    for (int w = 0; w < waves; ++w) {
-      const int k = s_count[w * nb + b];
-      s_count[w * nb + b] = tot;
-      tot += k;
+  // Twice over this wave's tokens: count them, and place them once everybody's counts are known.
+  for (int place = 0; place < 2; ++place) {
+    for (int t = t0; t < t1; t += 64 * kPlanBatch) {
+      if (place == 0 || per > 64 * kPlanBatch) load_ids(t);  // else they are still there
+      const int chunks = min((t1 - t + 63) >> 6, kPlanBatch);
+#pragma unroll 1
+      for (int i = 0; i < chunks; ++i) {
+        const int token = t + 64 * i + lane, key = s_ids[wave][64 * i + lane];
+        const bool on = token < t1;
+        const uint64_t m = same_key(key, bits, on);
+        const int before = __popcll(m & ((uint64_t(1) << lane) - 1));
+        const int at = on && before == 0 ? atomicAdd(mine + key, __popcll(m)) : 0;
+        if (place) {
+          const int rank = __shfl(at, __builtin_ctzll(m | (uint64_t(1) << 63))) + before;
+          const LoraFirst f = s_first[key];
+          if (on) {
+            out.tokens[f.tile() * kLoraTile + rank] = token;
+            if (rank == s_first[key + 1].pos() - f.pos() - 1) s_last[key] = token;
+          }
+        }
+      }
     }
-    s_start[b] = c[0], s_tile[b] = c[1], s_gtile[b] = c[2];
-    c[0] += tot;
-    c[1] += (tot + kLoraTile - 1) / kLoraTile;
-    if (b < n) c[2] += (tot + gtokens - 1) / gtokens;
-  }
-  int e[3];
-#pragma unroll
-  for (int q = 0; q < 3; ++q) {
-    e[q] = c[q];
+    __syncthreads();
+    if (place) break;
+    // Totals of a run of buckets per thread, scanned over the block; a wave's
+    // counts become its first position within the bucket.
+    const int run = (nb + NT - 1) / NT, b0 = min(tid * run, nb), b1 = min(b0 + run, nb);
+    LoraFirst c = {0, 0};
+    for (int b = b0; b < b1; ++b) {
+      int tot = 0;
+#pragma unroll 4
+      for (int w = 0; w < WAVES; ++w) {
+        const int k = s_count[w * nb + b];
+        s_count[w * nb + b] = tot;
+        tot += k;
+      }
+      s_first[b] = c;
+      auto tiles = [&](int len) { return uint64_t((tot + len - 1) / len); };
+      LoraFirst f = {uint64_t(tot) | tiles(kLoraTile) << 20, 0};
+      if (b < n) {
+        f.a |= tiles(kLoraGradTokens) << 34 | tiles(kLoraGradTokens * 2) << 48;
+        f.b = uint32_t(tiles(kLoraGradTokens * 4)) | uint32_t(tiles(kLoraGradTokens * 8)) << 16;
+      }
+      c.add(f);
+    }
+    LoraFirst e = c;
+#pragma unroll 1
     for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(e[q], d);
-      if (lane >= d) e[q] += up;
+      const LoraFirst up = {__shfl_up(e.a, d), uint32_t(__shfl_up(int(e.b), d))};
+      if (lane >= d) e.add(up);
     }
-    if (lane == 63) s_sum[q][wave] = e[q];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int q = 0; q < 3; ++q) {
-    e[q] -= c[q];
-    for (int w = 0; w < wave; ++w) e[q] += s_sum[q][w];
-  }
-  for (int b = b0; b < b1; ++b) s_start[b] += e[0], s_tile[b] += e[1], s_gtile[b] += e[2];
-  if (tid == NT - 1) {
-    s_start[nb] = T;
-    s_tile[nb] = e[1] + c[1];
-    s_gtile[nb] = e[2] + c[2];
-    head[0] = kLoraMagic, head[1] = T, head[2] = n, head[3] = e[1] + c[1], head[4] = e[2] + c[2];
-  }
-  __syncthreads();
-  for (int b = tid; b <= n; b += NT) gstart[b] = s_gtile[b];
-  for (int t = t0; t < t1; t += 64 * kPlanBatch) {
-    if (per > 64 * kPlanBatch) load_ids(t);  // else they are still there
-#pragma unroll
-    for (int i = 0; i < kPlanBatch; ++i) {
-      if (t + 64 * i >= t1) break;  // uniform
-      const bool on = t + 64 * i + lane < t1;
-      const int key = ids[i];
-      const uint64_t m = same_key(key, bits, on);
-      const uint64_t before = m & ((uint64_t(1) << lane) - 1);
-      const int at = on ? mine[key] : 0;
-      __builtin_amdgcn_wave_barrier();
-      if (on) tokens[s_tile[key] * kLoraTile + at + __popcll(before)] = t + 64 * i + lane;
-      if (on && before == 0) mine[key] += __popcll(m);
-      __builtin_amdgcn_wave_barrier();
+    if (lane == 63) s_sum[wave] = e;
+    __syncthreads();
+    e.a -= c.a, e.b -= c.b;
+#pragma unroll 1
+    for (int w = 0; w < wave; ++w) e.add(s_sum[w]);
+    for (int b = b0; b < b1; ++b) {
+      LoraFirst f = s_first[b];
+      f.add(e);
+      s_first[b] = f;
     }
+    if (tid == NT - 1) {
+      e.add(c);
+      s_first[nb] = e;
+      out.head[0] = kLoraMagic, out.head[1] = T, out.head[2] = n, out.head[3] = e.tile();
+#pragma unroll
+      for (int i = 0; i < kLoraGradLens; ++i) out.head[4 + i] = e.gtile(i);
+    }
+    __syncthreads();
   }
-  __syncthreads();
-  for (int b = wave; b < nb; b += waves) {
-    const int p = s_start[b], tot = s_start[b + 1] - p;
-    const int nt = s_tile[b + 1] - s_tile[b], ng = s_gtile[b + 1] - s_gtile[b];
-    if (tot == 0) continue;
+  for (int b = wave; b < nb; b += WAVES) {
+    const LoraFirst f = s_first[b], g = s_first[b + 1];
+    const int p = f.pos(), tot = g.pos() - p, nt = g.tile() - f.tile();
+#pragma unroll 1
     for (int i = lane; i < nt; i += 64)
-      tiles[s_tile[b] + i] = {p + i * kLoraTile, min(kLoraTile, tot - i * kLoraTile), b, 0};
-    for (int i = lane; i < ng; i += 64)
-      gtiles[s_gtile[b] + i] = {s_tile[b] + i * (gtokens / kLoraTile), min(gtokens, tot - i * gtokens), b, ng == 1};
-    int* slots = tokens + s_tile[b] * kLoraTile;
-    if (tot + lane < nt * kLoraTile) slots[tot + lane] = slots[tot - 1];
+      out.tiles[f.tile() + i] = {p + i * kLoraTile, min(kLoraTile, tot - i * kLoraTile), b, 0};
+    if (tot + lane < nt * kLoraTile) out.tokens[f.tile() * kLoraTile + tot + lane] = s_last[b];
+#pragma unroll 1
+    for (int l = 0; l < kLoraGradLens; ++l) {
+      const int len = kLoraGradTokens << l, ng = g.gtile(l) - f.gtile(l);
+      if (lane == 0) out.gstart[l][b] = f.gtile(l);
+#pragma unroll 1
+      for (int i = lane; i < ng; i += 64)
+        out.gtiles[l][f.gtile(l) + i] = {f.tile() + i * (len / kLoraTile), min(len, tot - i * len), b, ng == 1};
+    }
   }
 }
 
@@ -811,22 +837,21 @@ struct LoraGrad {
 template <int RT>
 constexpr int kGradStages = RT == 4 ? 3 : 4;
 
-// One block sums the products of up to 512 tokens of one adapter for 128
+// One block sums the products of up to 2048 tokens of one adapter for 128
 // columns and 16 RT ranks.  A stage of the pipeline is 32 tokens: their rows
 // of the tall matrix and the terms' fragments are copied into LDS two or three stages ahead, and
 // the rows come back transposed, so that the tokens become the contracted
 // index.  The waves split ranks and columns, never tokens, so no sum crosses a wave.
 // An adapter with one gradient tile is done; others leave partial sums.
 template <int RT, bool DB>
-__global__ __launch_bounds__(256) void lora_grad_kernel(LoraGrad a, LoraPlan plan) {
+__device__ __forceinline__ void lora_grad_body(const LoraGrad& a, const LoraPlan& plan, int block, u32x4 (*s_stage)[(8 + 3 * RT) * 64],
+                                               int* s_tok) {
   constexpr int NS = kGradStages<RT>;
   constexpr int NC = 2 * RT;                  // 16-column fragments per wave: 128 RT / 4 columns
   constexpr int COPIES = 8 + 3 * RT;          // 1 KiB each: 4 rows of 128 columns, or one fragment
   constexpr int PER = (COPIES + 3) / 4;       // per wave
-  __shared__ u32x4 s_stage[NS][COPIES * 64];
-  __shared__ int s_tok[512];
-  const int blocks = a.first[a.parts], gi = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
-  const LoraTile tile = plan.tile(plan.gtiles, gi, 4);
+  const int cbk = block % a.first[a.parts], gi = block / a.first[a.parts];
+  const LoraTile tile = plan.tile(plan.gtiles, gi, 4 + plan.glen);
   if (tile.count == 0) return;
   int part = 0;
   while (part + 1 < a.parts && cbk >= a.first[part + 1]) ++part;
@@ -896,6 +921,17 @@ __global__ __launch_bounds__(256) void lora_grad_kernel(LoraGrad a, LoraPlan pla
   }
 }
 
+// Both gradients in one launch where their ranks go in blocks of the same size: the blocks of dA, then dB's.
+template <int RT>
+__global__ __launch_bounds__(256, 2) void lora_grad_kernel(LoraGrad a, int blocksA, LoraGrad b, LoraPlan plan) {
+  __shared__ u32x4 s_stage[kGradStages<RT>][(8 + 3 * RT) * 64];
+  __shared__ int s_tok[kLoraGradMost];
+  if (int(blockIdx.x) < blocksA)
+    lora_grad_body<RT, false>(a, plan, blockIdx.x, s_stage, s_tok);
+  else
+    lora_grad_body<RT, true>(b, plan, blockIdx.x - blocksA, s_stage, s_tok);
+}
+
 // The gradients of adapters with several tiles from their partial sums, in the
 // tiles' order, and zeros for adapters that no token chose.
 __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float* __restrict__ partA, float* __restrict__ dA,
@@ -920,12 +956,13 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(const float* __restr
 hipError_t launch_lora_plan(const int* adapter, int T, int n, void* plan, hipStream_t s) {
   const LoraPlanLayout L = lora_plan_layout(T, n);
   int* w = static_cast<int*>(plan);
-  // 16 waves where their counts fit LDS beside the rest
-  const int waves = n <= 1024 ? kPlanMaxWaves : kPlanMaxWaves / 2;
-  const size_t lds = size_t(waves * (n + 1) + 3 * (n + 2)) * sizeof(int);
-  hipLaunchKernelGGL(lora_plan_kernel, dim3(1), dim3(64 * waves), lds, s, adapter, T, n, lora_grad_tokens(T), w,
-                     reinterpret_cast<LoraTile*>(w + L.tiles), w + L.tokens, reinterpret_cast<LoraTile*>(w + L.gtiles),
-                     w + L.gstart);
+  LoraPlanOut out = {w, reinterpret_cast<LoraTile*>(w + L.tiles), w + L.tokens, {}, {}};
+  for (int i = 0; i < kLoraGradLens; ++i)
+    out.gtiles[i] = reinterpret_cast<LoraTile*>(w + L.gtiles[i]), out.gstart[i] = w + L.gstart[i];
+  const int waves = n <= 1024 ? 16 : 8;  // whose counts fit LDS
+  const size_t lds = size_t(waves * (n + 1) + 1) * sizeof(int) + size_t(n + 2) * sizeof(LoraFirst) + size_t(n + 1) * sizeof(int);
+  if (waves == 16) hipLaunchKernelGGL(lora_plan_kernel<16>, dim3(1), dim3(1024), lds, s, adapter, T, n, out);
+  else hipLaunchKernelGGL(lora_plan_kernel<8>, dim3(1), dim3(512), lds, s, adapter, T, n, out);
   return hipGetLastError();
 }
 
@@ -970,7 +1007,7 @@ static hipError_t launch_up(LoraUp& u, int ranks, int tiles, const LoraPlan& pla
 hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, const float* scale,
                            const void* plan, const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* Y,
                            int64_t ldy, float* P, float* part, int splits, hipStream_t s) {
-  const LoraPlan pl = lora_plan(plan, z.T, z.n);
+  const LoraPlan pl = lora_plan(plan, z.T, z.n, 0);
   const int R = z.parts * z.r, tiles = lora_max_tiles(z);
   LoraDown d = {};
   d.X = X, d.ldx = ldx, d.W = A, d.wstride = int64_t(R) * z.d_in, d.K = z.d_in, d.wrows = R;
@@ -988,25 +1025,36 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   return launch_up<false>(u, z.r, tiles, pl, s);
 }
 
-template <bool DB>
-static hipError_t launch_grad(const LoraGrad& a, const LoraPlan& plan, int gtiles, hipStream_t s) {
-  const int rt = rank_tiles(a.r);
-  const dim3 grid(unsigned(gtiles) * unsigned(a.first[a.parts]), unsigned((a.r + 16 * rt - 1) / (16 * rt))), block(256);
+static hipError_t launch_grad(const LoraGrad& a, const LoraGrad& b, int ranks, const LoraPlan& plan, int gtiles,
+                              hipStream_t s) {
+  const int rt = rank_tiles(ranks), blocksA = gtiles * a.first[a.parts], blocksB = gtiles * b.first[b.parts];
+  const dim3 grid(unsigned(blocksA) + unsigned(blocksB), unsigned((ranks + 16 * rt - 1) / (16 * rt))), block(256);
   switch (rt) {
-    case 1: hipLaunchKernelGGL((lora_grad_kernel<1, DB>), grid, block, 0, s, a, plan); break;
-    case 2: hipLaunchKernelGGL((lora_grad_kernel<2, DB>), grid, block, 0, s, a, plan); break;
-    default: hipLaunchKernelGGL((lora_grad_kernel<4, DB>), grid, block, 0, s, a, plan); break;
+    case 1: hipLaunchKernelGGL(lora_grad_kernel<1>, grid, block, 0, s, a, blocksA, b, plan); break;
+    case 2: hipLaunchKernelGGL(lora_grad_kernel<2>, grid, block, 0, s, a, blocksA, b, plan); break;
+    default: hipLaunchKernelGGL(lora_grad_kernel<4>, grid, block, 0, s, a, blocksA, b, plan); break;
   }
   return hipGetLastError();
+}
+
+int lora_bwd_glen(const LoraShape& z) {
+  int64_t blocks = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
+  for (int p = 0; p < z.parts; ++p) blocks += (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
+  if (z.parts > 1) {  // two launches
+    const int64_t a = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
+    blocks = a < blocks - a ? a : blocks - a;
+  }
+  return lora_grad_len(z.T, blocks);
 }
 
 hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64_t ldx, const uint16_t* A,
                            const uint16_t* B, const float* scale, const void* plan, const float* P,
                            const LoraShape& z, const uint16_t* base, int64_t ld_base, uint16_t* dX, int64_t lddx,
                            float* dA, float* dB, const LoraBwdWs& w, int splits, hipStream_t s) {
-  const LoraPlan pl = lora_plan(plan, z.T, z.n);
   const LoraPlanLayout L = lora_plan_layout(z.T, z.n);
-  const int R = z.parts * z.r, tiles = int(L.max_tiles), gtiles = int(L.max_gtiles);
+  const int glen = lora_bwd_glen(z);
+  const LoraPlan pl = lora_plan(plan, z.T, z.n, glen);
+  const int R = z.parts * z.r, tiles = int(L.max_tiles), gtiles = int(L.max_gtiles[glen]);
   int off[kLoraMaxParts] = {}, widest = 0;
   for (int p = 0, at = 0; p < z.parts; ++p) {
     off[p] = at;
@@ -1035,22 +1083,27 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
     u.Qn = w.Qn, u.blocksQ = m.blocksQ, u.parts = 1, u.width[0] = z.d_in;
     if ((e = launch_up<true>(u, R, tiles, pl, s))) return e;
   }
-  LoraGrad g = {};
+  LoraGrad ga = {}, gb = {}, none = {};
   if (dA) {
-    g.X = X, g.ldx = ldx, g.terms = w.Qt, g.tblocks = g.pblocks = m.blocksQ, g.r = R;
-    g.out = dA, g.ostride = int64_t(R) * z.d_in, g.ocols = z.d_in, g.part = w.partA, g.parts = 1, g.width[0] = z.d_in;
-    g.first[1] = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
-    if ((e = launch_grad<false>(g, pl, gtiles, s))) return e;
+    ga.X = X, ga.ldx = ldx, ga.terms = w.Qt, ga.tblocks = ga.pblocks = m.blocksQ, ga.r = R;
+    ga.out = dA, ga.ostride = int64_t(R) * z.d_in, ga.ocols = z.d_in, ga.part = w.partA, ga.parts = 1;
+    ga.width[0] = z.d_in;
+    ga.first[1] = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
   }
   if (dB) {
-    g.X = dY, g.ldx = lddy, g.terms = w.Pt, g.tblocks = m.blocksP, g.pblocks = m.blocksP / z.parts, g.r = z.r;
-    g.scale = scale, g.out = dB, g.ostride = int64_t(z.d_out) * z.r, g.ocols = z.d_out, g.part = w.partB;
-    g.parts = z.parts;
+    gb.X = dY, gb.ldx = lddy, gb.terms = w.Pt, gb.tblocks = m.blocksP, gb.pblocks = m.blocksP / z.parts, gb.r = z.r;
+    gb.scale = scale, gb.out = dB, gb.ostride = int64_t(z.d_out) * z.r, gb.ocols = z.d_out, gb.part = w.partB;
+    gb.parts = z.parts;
     for (int p = 0; p < z.parts; ++p) {
-      g.off[p] = off[p], g.width[p] = z.widths[p];
-      g.first[p + 1] = g.first[p] + (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
+      gb.off[p] = off[p], gb.width[p] = z.widths[p];
+      gb.first[p + 1] = gb.first[p] + (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
     }
-    if ((e = launch_grad<true>(g, pl, gtiles, s))) return e;
+  }
+  if (z.parts == 1 && (dA || dB)) {
+    if ((e = launch_grad(ga, gb, R, pl, gtiles, s))) return e;
+  } else {
+    if (dA && (e = launch_grad(ga, none, R, pl, gtiles, s))) return e;
+    if (dB && (e = launch_grad(none, gb, z.r, pl, gtiles, s))) return e;
   }
   if (dA || dB) {
     const int64_t sA = int64_t(R) * z.d_in, sB = int64_t(z.d_out) * z.r;
