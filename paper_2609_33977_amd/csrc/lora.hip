@@ -150,17 +150,19 @@ __global__ __launch_bounds__(64 * WAVES) void lora_plan_kernel(const int* __rest
     }
     __syncthreads();
     if (place) break;
-    // Totals of a run of buckets per thread, scanned over the block; a wave's
+    // Totals of a run of buckets per thread, scanned over the threads that have any; a wave's
     // counts become its first position within the bucket.
     const int run = (nb + NT - 1) / NT, b0 = min(tid * run, nb), b1 = min(b0 + run, nb);
     LoraFirst c = {0, 0};
     for (int b = b0; b < b1; ++b) {
       int tot = 0;
-#pragma unroll 4
+      int k[WAVES];
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) k[w] = s_count[w * nb + b];
+#pragma unroll
       for (int w = 0; w < WAVES; ++w) {
-        const int k = s_count[w * nb + b];
         s_count[w * nb + b] = tot;
-        tot += k;
+        tot += k[w];
       }
       s_first[b] = c;
       auto tiles = [&](int len) { return uint64_t((tot + len - 1) / len); };
@@ -173,21 +175,23 @@ __global__ __launch_bounds__(64 * WAVES) void lora_plan_kernel(const int* __rest
     }
     LoraFirst e = c;
 #pragma unroll 1
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < min(64, nb); d <<= 1) {
       const LoraFirst up = {__shfl_up(e.a, d), uint32_t(__shfl_up(int(e.b), d))};
       if (lane >= d) e.add(up);
     }
     if (lane == 63) s_sum[wave] = e;
     __syncthreads();
     e.a -= c.a, e.b -= c.b;
+    if (b0 < b1) {
 #pragma unroll 1
-    for (int w = 0; w < wave; ++w) e.add(s_sum[w]);
+      for (int w = 0; w < wave; ++w) e.add(s_sum[w]);
+    }
     for (int b = b0; b < b1; ++b) {
       LoraFirst f = s_first[b];
       f.add(e);
       s_first[b] = f;
     }
-    if (tid == NT - 1) {
+    if (b0 < b1 && b1 == nb) {
       e.add(c);
       s_first[nb] = e;
       out.head[0] = kLoraMagic, out.head[1] = T, out.head[2] = n, out.head[3] = e.tile();
@@ -196,20 +200,24 @@ __global__ __launch_bounds__(64 * WAVES) void lora_plan_kernel(const int* __rest
     }
     __syncthreads();
   }
-  for (int b = wave; b < nb; b += WAVES) {
+  // 16 lanes per bucket
+  const int l16 = tid & 15;
+#pragma unroll 1
+  for (int b = tid >> 4; b < nb; b += NT / 16) {
     const LoraFirst f = s_first[b], g = s_first[b + 1];
     const int p = f.pos(), tot = g.pos() - p, nt = g.tile() - f.tile();
 #pragma unroll 1
-    for (int i = lane; i < nt; i += 64)
+    for (int i = l16; i < nt; i += 16)
       out.tiles[f.tile() + i] = {p + i * kLoraTile, min(kLoraTile, tot - i * kLoraTile), b, 0};
-    if (tot + lane < nt * kLoraTile) out.tokens[f.tile() * kLoraTile + tot + lane] = s_last[b];
 #pragma unroll 1
+    for (int i = tot + l16; i < nt * kLoraTile; i += 16) out.tokens[f.tile() * kLoraTile + i] = s_last[b];
+#pragma unroll
     for (int l = 0; l < kLoraGradLens; ++l) {
-      const int len = kLoraGradTokens << l, ng = g.gtile(l) - f.gtile(l);
-      if (lane == 0) out.gstart[l][b] = f.gtile(l);
+      const int len = kLoraGradTokens << l, first = f.gtile(l), ng = g.gtile(l) - first;
+      if (l16 == 0) out.gstart[l][b] = first;
 #pragma unroll 1
-      for (int i = lane; i < ng; i += 64)
-        out.gtiles[l][f.gtile(l) + i] = {f.tile() + i * (len / kLoraTile), min(len, tot - i * len), b, ng == 1};
+      for (int i = l16; i < ng; i += 16)
+        out.gtiles[l][first + i] = {f.tile() + i * (len / kLoraTile), min(len, tot - i * len), b, ng == 1};
     }
   }
 }
