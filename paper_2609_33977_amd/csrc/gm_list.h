@@ -1,5 +1,7 @@
 // Layout of a tensor list in device memory: a header, one entry per tensor,
-// and the tensor of every chunk of kListChunk values.
+// and the tensor of every chunk of kListChunk values.  A tensor's chunks begin
+// where its gradient is 16-byte aligned; the few values before that (its head)
+// belong to the first.
 #pragma once
 
 #include <stddef.h>
@@ -10,7 +12,7 @@ namespace gm {
 constexpr int kListChunk = 8192;
 constexpr int kListPerLaunch = 48;  // entries that one launch carries in its arguments
 constexpr int32_t kListMagic = 0x4c9e21b7;
-constexpr int kListVector = 1, kListGradBf16 = 2;  // entry flags
+constexpr int kListVector = 1, kListGradBf16 = 2, kListHeadShift = 8;  // entry flags, and the head's values from bit 8 up
 constexpr int kNormBlocks = 2048;
 
 struct ListHead {

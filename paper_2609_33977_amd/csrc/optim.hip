@@ -65,51 +65,72 @@ __device__ __forceinline__ double sum_block(double v) {
   return (s_w[0] + s_w[1]) + (s_w[2] + s_w[3]);
 }
 
+__device__ __forceinline__ double add_squares(double sum, const f32x4& v) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) sum = fma(double(v[q]), double(v[q]), sum);
+  return sum;
+}
+
+__device__ __forceinline__ double add_squares(double sum, const u32x4& v) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const double a = bf16_lo(v[q]), b = bf16_hi(v[q]);
+    sum = fma(a, a, sum);
+    sum = fma(b, b, sum);
+  }
+  return sum;
+}
+
+// A chunk's values: [start, end), of which those before `body` are the tensor's head.
+struct ListRange {
+  int64_t start, body, end;
+  __device__ __forceinline__ ListRange(const ListEntry& e, int chunk) {
+    const int64_t k = chunk - e.first, head = e.flags >> kListHeadShift;
+    body = min(head + k * kListChunk, e.numel);
+    end = min(head + (k + 1) * kListChunk, e.numel);
+    start = k == 0 ? 0 : body;
+  }
+};
+
+__device__ __forceinline__ double square_of(float g) { return double(g) * double(g); }
+__device__ __forceinline__ double square_of(uint16_t g) { return square_of(bf16_to_f32(g)); }
+
+// A chunk's squares, by 16-byte vectors of type V; a whole chunk has all its loads in flight.
+template <typename V, typename T>
+__device__ __forceinline__ double chunk_squares(double sum, const ListEntry& e, int chunk) {
+  constexpr int PER = 16 / sizeof(T), N = kListChunk / (256 * PER);
+  const ListRange r(e, chunk);
+  const T* g = static_cast<const T*>(e.g) + r.body;
+  const int len = int(r.end - r.body);
+  if (r.start + threadIdx.x < r.body) sum += square_of(static_cast<const T*>(e.g)[r.start + threadIdx.x]);
+  if (len == kListChunk) {
+    V v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const V*>(g) + i * 256 + threadIdx.x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum = add_squares(sum, v[i]);
+    return sum;
+  }
+  const int done = len / PER * PER;
+  for (int i = PER * threadIdx.x; i < done; i += 256 * PER) sum = add_squares(sum, *reinterpret_cast<const V*>(g + i));
+  if (done + int(threadIdx.x) < len) sum += square_of(g[done + threadIdx.x]);
+  return sum;
+}
+
 // Squares are summed in fp64: the square of an fp32 value is exact there and
-// cannot overflow.
+// cannot overflow.  The next chunk's entry is loaded while this one's values are.
 __global__ __launch_bounds__(256) void grad_norm_kernel(const void* list, size_t bytes, double* __restrict__ part) {
   double sum = 0.0;
   const ListView L(list, bytes);
+  ListEntry next;
+  if (int(blockIdx.x) < L.chunks) next = L.entries[L.map[blockIdx.x]];
   for (int c = blockIdx.x; c < L.chunks; c += gridDim.x) {
-    const ListEntry e = L.entries[L.map[c]];
-    const int64_t at = int64_t(c - e.first) * kListChunk;
-    const int len = int(min(e.numel - at, int64_t(kListChunk)));
-    if (e.flags & kListGradBf16) {
-      const uint16_t* g = static_cast<const uint16_t*>(e.g) + at;
-      int done = 0;
-      if (e.flags & kListVector) {
-        done = len / 8 * 8;
-        for (int i = 8 * threadIdx.x; i < done; i += 2048) {
-          const u32x4 v = ld16(g + i);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const double a = bf16_lo(v[q]), b = bf16_hi(v[q]);
-            sum = fma(a, a, sum);
-            sum = fma(b, b, sum);
-          }
-        }
-      }
-      for (int i = done + threadIdx.x; i < len; i += 256) {
-        const double a = bf16_to_f32(g[i]);
-        sum = fma(a, a, sum);
-      }
-    } else {
-      const float* g = static_cast<const float*>(e.g) + at;
-      int done = 0;
-      if (e.flags & kListVector) {
-        done = len / 4 * 4;
-#pragma unroll 8
-        for (int i = 4 * threadIdx.x; i < done; i += 1024) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(g + i);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) sum = fma(double(v[q]), double(v[q]), sum);
-        }
-      }
-      for (int i = done + threadIdx.x; i < len; i += 256) {
-        const double a = g[i];
-        sum = fma(a, a, sum);
-      }
-    }
+    const ListEntry e = next;
+    if (c + int(gridDim.x) < L.chunks) next = L.entries[L.map[c + gridDim.x]];
+    if (e.flags & kListGradBf16)
+      sum = chunk_squares<u32x4, uint16_t>(sum, e, c);
+    else
+      sum = chunk_squares<f32x4, float>(sum, e, c);
   }
   const double s = sum_block(sum);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -134,49 +155,51 @@ __global__ __launch_bounds__(256) void adamw_list_kernel(const void* list, size_
   for (int c = blockIdx.x; c < L.chunks; c += gridDim.x) {
     const ListEntry e = L.entries[L.map[c]];
     if (!e.p || !e.m || !e.v) continue;
-    const int64_t at = int64_t(c - e.first) * kListChunk;
-    const int len = int(min(e.numel - at, int64_t(kListChunk)));
-    float *p = e.p + at, *m = e.m + at, *v = e.v + at;
-    uint16_t* h = e.p16 ? e.p16 + at : nullptr;
+    const ListRange r(e, c);
     const bool b16 = e.flags & kListGradBf16;
-    const float* g = b16 ? nullptr : static_cast<const float*>(e.g) + at;
-    const uint16_t* gh = b16 ? static_cast<const uint16_t*>(e.g) + at : nullptr;
-    int done = 0;
-    if (e.flags & kListVector) {
-      done = len / 4 * 4;
-      for (int i = 4 * threadIdx.x; i < done; i += 1024) {
-        f32x4 pv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p + i));
-        f32x4 mv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(m + i));
-        f32x4 vv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(v + i));
-        f32x4 gv;
-        if (b16) {
-          const uint64_t w = *reinterpret_cast<const uint64_t*>(gh + i);
+    const float* g = static_cast<const float*>(e.g);
+    const uint16_t* gh = static_cast<const uint16_t*>(e.g);
+    auto one = [&](int64_t i) {
+      float mq = e.m[i], vq = e.v[i];
+      const float w = opt.step(e.p[i], (b16 ? bf16_to_f32(gh[i]) : g[i]) * k, mq, vq);
+      e.p[i] = w, e.m[i] = mq, e.v[i] = vq;
+      if (e.p16) e.p16[i] = uint16_t(f32_to_bf16_bits(w));
+    };
+    if (!(e.flags & kListVector)) {
+      for (int64_t i = r.start + threadIdx.x; i < r.end; i += 256) one(i);
+      continue;
+    }
+    if (r.start + threadIdx.x < r.body) one(r.start + threadIdx.x);
+    const int64_t done = r.body + (r.end - r.body) / 4 * 4;
+    // Everything streams through once: nontemporal, as in the flat step.
+#pragma unroll 2
+    for (int64_t i = r.body + 4 * threadIdx.x; i < done; i += 1024) {
+      f32x4 pv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.p + i));
+      f32x4 mv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.m + i));
+      f32x4 vv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.v + i));
+      f32x4 gv;
+      if (b16) {
+        const uint64_t w = *reinterpret_cast<const uint64_t*>(gh + i);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) gv[q] = bf16_to_f32(uint16_t(w >> (16 * q)));
-        } else {
-          gv = *reinterpret_cast<const f32x4*>(g + i);
-        }
+        for (int q = 0; q < 4; ++q) gv[q] = bf16_to_f32(uint16_t(w >> (16 * q)));
+      } else {
+        gv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(g + i));
+      }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float mq = mv[q], vq = vv[q];
-          pv[q] = opt.step(pv[q], gv[q] * k, mq, vq);
-          mv[q] = mq, vv[q] = vq;
-        }
-        __builtin_nontemporal_store(pv, reinterpret_cast<f32x4*>(p + i));
-        __builtin_nontemporal_store(mv, reinterpret_cast<f32x4*>(m + i));
-        __builtin_nontemporal_store(vv, reinterpret_cast<f32x4*>(v + i));
-        if (h) {
-          const uint64_t w = uint64_t(pack_bf16x2(pv[0], pv[1])) | uint64_t(pack_bf16x2(pv[2], pv[3])) << 32;
-          *reinterpret_cast<uint64_t*>(h + i) = w;
-        }
+      for (int q = 0; q < 4; ++q) {
+        float mq = mv[q], vq = vv[q];
+        pv[q] = opt.step(pv[q], gv[q] * k, mq, vq);
+        mv[q] = mq, vv[q] = vq;
+      }
+      __builtin_nontemporal_store(pv, reinterpret_cast<f32x4*>(e.p + i));
+      __builtin_nontemporal_store(mv, reinterpret_cast<f32x4*>(e.m + i));
+      __builtin_nontemporal_store(vv, reinterpret_cast<f32x4*>(e.v + i));
+      if (e.p16) {
+        const uint64_t w = uint64_t(pack_bf16x2(pv[0], pv[1])) | uint64_t(pack_bf16x2(pv[2], pv[3])) << 32;
+        __builtin_nontemporal_store(w, reinterpret_cast<uint64_t*>(e.p16 + i));
       }
     }
-    for (int i = done + threadIdx.x; i < len; i += 256) {
-      float mq = m[i], vq = v[i];
-      const float w = opt.step(p[i], (b16 ? bf16_to_f32(gh[i]) : g[i]) * k, mq, vq);
-      p[i] = w, m[i] = mq, v[i] = vq;
-      if (h) h[i] = uint16_t(f32_to_bf16_bits(w));
-    }
+    if (done + threadIdx.x < r.end) one(done + threadIdx.x);
   }
 }
 
@@ -203,9 +226,12 @@ hipError_t launch_tensor_list(float* const* p, const void* const* g, float* cons
       e.numel = numel[t];
       e.first = first;
       const bool b16 = g_bf16 && g_bf16[t];
-      // Vectors of four values (eight bf16 gradients in the norm) where every address allows them.
-      const bool vec = aligned(e.g, 16) && aligned(e.p, 16) && aligned(e.m, 16) && aligned(e.v, 16) && aligned(e.p16, 8);
-      e.flags = (b16 ? kListGradBf16 : 0) | (vec ? kListVector : 0);
+      // Values before the gradient's first 16-byte boundary, and whether the step's vectors of four fit the other
+      // addresses there too (tensors cut alike from one buffer per role have them in the same place).
+      const uintptr_t size = b16 ? 2 : 4, head = ((16 - reinterpret_cast<uintptr_t>(e.g)) & 15) / size;
+      const bool vec = aligned(e.p + head, 16) && aligned(e.m + head, 16) && aligned(e.v + head, 16) &&
+                       (!e.p16 || aligned(e.p16 + head, 8));
+      e.flags = (b16 ? kListGradBf16 : 0) | (e.p && vec ? kListVector : 0) | int(head) << kListHeadShift;
       w.index[i] = t;
       w.chunks[i] = int(list_chunks(numel[t]));
       first += w.chunks[i];
