@@ -171,19 +171,20 @@ __global__ __launch_bounds__(256) void adamw_list_kernel(const void* list, size_
     }
     if (r.start + threadIdx.x < r.body) one(r.start + threadIdx.x);
     const int64_t done = r.body + (r.end - r.body) / 4 * 4;
-    // Everything streams through once: nontemporal, as in the flat step.
+    // Plain loads and nontemporal stores: parameters and moments of 2 to 15 M values, which stay in the last-level
+    // cache from step to step, at 4.7 to 6.0 TB/s (3.9 to 5.1 with nontemporal loads too), 48 M at 5.1 (5.3).
 #pragma unroll 2
     for (int64_t i = r.body + 4 * threadIdx.x; i < done; i += 1024) {
-      f32x4 pv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.p + i));
-      f32x4 mv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.m + i));
-      f32x4 vv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(e.v + i));
+      f32x4 pv = *reinterpret_cast<const f32x4*>(e.p + i);
+      f32x4 mv = *reinterpret_cast<const f32x4*>(e.m + i);
+      f32x4 vv = *reinterpret_cast<const f32x4*>(e.v + i);
       f32x4 gv;
       if (b16) {
         const uint64_t w = *reinterpret_cast<const uint64_t*>(gh + i);
 #pragma unroll
         for (int q = 0; q < 4; ++q) gv[q] = bf16_to_f32(uint16_t(w >> (16 * q)));
       } else {
-        gv = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(g + i));
+        gv = *reinterpret_cast<const f32x4*>(g + i);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
