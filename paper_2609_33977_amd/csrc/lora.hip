@@ -990,13 +990,17 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
 // Blocks of 16, 32 or 64 ranks.
 static int rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
 
-// Blocks of up to 1024 columns: the rank terms and the plan cost less per column, down to 256 where there are few tiles.
+// Blocks of up to 1024 columns, down to 256 where there are few tiles: four blocks per CU to hide latency (4099
+// tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
+// terms that every block stages count for more: high ranks (8192 tokens, 4096 columns, 64 ranks: 36 with two, 43 with
+// four) and tiles of few tokens (64 tokens of 32 adapters, 15360 columns, 16 ranks: 9.0 and 11.4).
 template <bool TR>
 static hipError_t launch_up(LoraUp& u, int ranks, int tiles, const LoraPlan& plan, hipStream_t s) {
   int cols = 0;
   for (int p = 0; p < u.parts; ++p) cols += u.width[p];
+  const int want = TR || (ranks <= 32 && plan.T >= tiles * (kLoraTile / 2)) ? 1024 : 512;
   u.span = 1024;
-  while (u.span > 256 && int64_t(tiles) * (cols / u.span) < 512) u.span /= 2;
+  while (u.span > 256 && int64_t(tiles) * (cols / u.span) < want) u.span /= 2;
   if (ranks > 128) u.span = kUpCols<8>;
   for (int p = 0, off = 0; p < u.parts; ++p) {
     u.off[p] = off;
