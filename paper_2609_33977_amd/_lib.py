@@ -392,31 +392,50 @@ def gm_adamw(p, g, m, v, lr: float, beta1: float, beta2: float, eps: float, weig
 GM_LORA_MAX_PARTS = 4
 
 
-def _rows(where, what, t, cols, rows):
+# One call checks a tensor and takes its pointer: every call of a decode step
+# pays for it (the checks of gm_lora_fwd took 6.5 us one by one, against 8 of its kernels).
+
+_BF16, _F32, _U8 = torch.bfloat16, torch.float32, torch.uint8
+_current_device = _raw_device or torch.cuda.current_device
+
+
+def _device():
+    """The current device, which every tensor of a call has to be on."""
+    return _current_device() if torch.cuda.is_initialized() else -2
+
+
+def _on(where, what, t, dtype, shape, dev):
+    """Pointer of a contiguous tensor of that dtype and shape (None: any) on device dev."""
+    if (t is not None and t.dtype is dtype and (shape is None or t.shape == shape) and t.is_contiguous()
+            and t.get_device() == dev):
+        return t.data_ptr()
+    _refuse(where, what, t, dtype, shape, dev)
+
+
+def _refuse(where, what, t, dtype, shape, dev):
+    if t is None:
+        raise ValueError(f"{where}: {what} is required")
+    if t.dtype is not dtype:
+        raise ValueError(f"{where}: {what} must be {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{where}: {what} must have shape {shape}, got {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: {what} must live on the current GPU, got {t.device}")
+    raise ValueError(f"{where}: {what} must be contiguous")
+
+
+def _rows(where, what, t, shape, dev):
     """Pointer and row stride of a bf16 matrix that may be columns of a wider one."""
-    if t.dtype is not torch.bfloat16:
-        raise ValueError(f"{where}: {what} must be {torch.bfloat16}, got {t.dtype}")
-    have = t.shape
-    if len(have) != 2 or have[0] != rows or have[1] != cols:
-        raise ValueError(f"{where}: {what} must have shape {(rows, cols)}, got {tuple(have)}")
+    if t is None or t.dtype is not _BF16 or t.shape != shape or t.get_device() != dev:
+        _refuse(where, what, t, _BF16, shape, dev)
     ld, one = t.stride()
-    if rows == 1 or ld == 0:  # one row's stride means nothing; rows that share memory are no matrix
-        if rows > 1:
-            raise ValueError(f"{where}: {what} repeats one row")
-        ld = cols
-    if one != 1 and cols > 1:
+    if one != 1 and shape[1] > 1:
         raise ValueError(f"{where}: {what} must have contiguous rows")
-    if not t.is_cuda:
-        raise ValueError(f"{where}: {what} must live on the GPU")
+    if shape[0] == 1:  # one row's stride means nothing
+        ld = shape[1]
+    elif ld < shape[1]:
+        raise ValueError(f"{where}: the rows of {what} overlap")
     return t.data_ptr(), ld
-
-
-def _one_device(where, *tensors):
-    """The kernels run on the current device: every tensor has to be there."""
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{where}: every tensor must live on the current device {dev}, got one on {t.device}")
 
 
 _WIDTHS = {}  # the C arrays of the few width lists that a model has
@@ -453,24 +472,24 @@ def gm_lora_workspace_size(op: int, T: int, n: int, d_in: int, widths, r: int) -
 def gm_lora_plan(adapter, n: int, plan, stream=None) -> None:
     """Sorts the tokens of a batch by adapter (see gm_lora_plan in the header); adapter [T] int32."""
     w = "gm_lora_plan"
-    _arg(w, "adapter", adapter, "i32", shape=(None,))
-    _arg(w, "plan", plan, "u8")
-    a, p = _ptr(adapter), _ptr(plan)
-    _one_device(w, adapter, plan)
+    if adapter.dim() != 1:
+        raise ValueError(f"{w}: adapter must have shape (T,), got {tuple(adapter.shape)}")
+    dev = _device()
+    a, p = _on(w, "adapter", adapter, torch.int32, None, dev), _on(w, "plan", plan, _U8, None, dev)
     _check(LIB.gm_lora_plan(a, adapter.shape[0], int(n), p, plan.numel(), _stream(stream)), w)
 
 
-def _adapters(w, A, B, scale, widths):
-    """(n, d_in, d_out, parts, r, C array of widths) of a pool."""
-    _arg(w, "A", A, "bf16", shape=(None, None, None))
+def _adapters(w, X, A, B, widths):
+    """(T, n, R, d_in, d_out, r, C array of widths) of tokens and a pool, whose dtypes are checked with their pointers."""
+    if X.dim() != 2 or A.dim() != 3 or B.dim() != 3:
+        raise ValueError(f"{w}: X must be [T, d_in], A [n, ranks, d_in] and B [n, d_out, r], got {tuple(X.shape)}, "
+                         f"{tuple(A.shape)} and {tuple(B.shape)}")
     n, R, d_in = A.shape
-    _arg(w, "B", B, "bf16", shape=(n, None, None))
-    d_out, r = B.shape[1], B.shape[2]
+    nb, d_out, r = B.shape
     parts = _widths(w, widths, d_out)
-    if R != len(parts) * r:
-        raise ValueError(f"{w}: A must hold {len(parts)} x {r} ranks, got {R}")
-    _arg(w, "scale", scale, "f32", numel=n)
-    return n, R, d_in, d_out, r, parts
+    if nb != n or R != len(parts) * r:
+        raise ValueError(f"{w}: A {tuple(A.shape)} and B {tuple(B.shape)} are no pool of {len(parts)} projections")
+    return X.shape[0], n, R, d_in, d_out, r, parts
 
 
 def gm_lora_fwd(X, A, B, scale, plan, base, Y, P=None, ws=None, widths=None, stream=None) -> None:
@@ -478,43 +497,40 @@ def gm_lora_fwd(X, A, B, scale, plan, base, Y, P=None, ws=None, widths=None, str
 
     X, base and Y may be columns of wider buffers; widths are those of stacked projections (None: one)."""
     w = "gm_lora_fwd"
-    n, R, d_in, d_out, r, parts = _adapters(w, A, B, scale, widths)
-    T = X.shape[0]
-    _arg(w, "P", P, "f32", shape=(T, R), optional=True)
-    _arg(w, "plan", plan, "u8")
-    _arg(w, "ws", ws, "u8")
-    x, ldx = _rows(w, "X", X, d_in, T)
-    b, ldb = _rows(w, "base", base, d_out, T)
-    y, ldy = _rows(w, "Y", Y, d_out, T)
-    _one_device(w, X, A, B, scale, plan, base, Y, P, ws)
-    _check(LIB.gm_lora_fwd(x, ldx, _ptr(A), _ptr(B), _ptr(scale), _ptr(plan), plan.numel(), T, n, d_in, parts,
-                           len(parts), r, b, ldb, y, ldy, _ptr(P), _ptr(ws), ws.numel(), _stream(stream)), w)
+    T, n, R, d_in, d_out, r, parts = _adapters(w, X, A, B, widths)
+    dev = _device()
+    x, ldx = _rows(w, "X", X, (T, d_in), dev)
+    b, ldb = _rows(w, "base", base, (T, d_out), dev)
+    y, ldy = _rows(w, "Y", Y, (T, d_out), dev)
+    p = None if P is None else _on(w, "P", P, _F32, (T, R), dev)
+    _check(LIB.gm_lora_fwd(x, ldx, _on(w, "A", A, _BF16, None, dev), _on(w, "B", B, _BF16, None, dev),
+                           _on(w, "scale", scale, _F32, (n,), dev), _on(w, "plan", plan, _U8, None, dev), plan.numel(), T,
+                           n, d_in, parts, len(parts), r, b, ldb, y, ldy, p, _on(w, "ws", ws, _U8, None, dev),
+                           ws.numel(), _stream(stream)), w)
 
 
 def gm_lora_bwd(dY, X, A, B, scale, plan, P, base=None, dX=None, dA=None, dB=None, ws=None, widths=None,
                 stream=None) -> None:
     """Gradients of the adapters and of their input (see gm_lora_bwd in the header); P, base only as the outputs need."""
     w = "gm_lora_bwd"
-    n, R, d_in, d_out, r, parts = _adapters(w, A, B, scale, widths)
-    T = X.shape[0]
-    _arg(w, "P", P, "f32", shape=(T, R), optional=dB is None)
-    _arg(w, "dA", dA, "f32", shape=(n, R, d_in), optional=True)
-    _arg(w, "dB", dB, "f32", shape=(n, d_out, r), optional=True)
-    _arg(w, "plan", plan, "u8")
-    _arg(w, "ws", ws, "u8")
-    y, ldy = _rows(w, "dY", dY, d_out, T)
-    x, ldx = _rows(w, "X", X, d_in, T)
-    b = dx = None
+    T, n, R, d_in, d_out, r, parts = _adapters(w, X, A, B, widths)
+    dev = _device()
+    y, ldy = _rows(w, "dY", dY, (T, d_out), dev)
+    x, ldx = _rows(w, "X", X, (T, d_in), dev)
+    b = dx = p = da = db = None
     ldb = lddx = d_in
     if dX is not None:
-        if base is None:
-            raise ValueError(f"{w}: base is required")
-        b, ldb = _rows(w, "base", base, d_in, T)
-        dx, lddx = _rows(w, "dX", dX, d_in, T)
-    _one_device(w, dY, X, A, B, scale, plan, P, base, dX, dA, dB, ws)
-    _check(LIB.gm_lora_bwd(y, ldy, x, ldx, _ptr(A), _ptr(B), _ptr(scale), _ptr(plan), plan.numel(), _ptr(P), T, n,
-                           d_in, parts, len(parts), r, b, ldb, dx, lddx, _ptr(dA), _ptr(dB), _ptr(ws), ws.numel(),
-                           _stream(stream)), w)
+        b, ldb = _rows(w, "base", base, (T, d_in), dev)
+        dx, lddx = _rows(w, "dX", dX, (T, d_in), dev)
+    if dA is not None:
+        da = _on(w, "dA", dA, _F32, A.shape, dev)
+    if dB is not None:
+        db = _on(w, "dB", dB, _F32, B.shape, dev)
+        p = _on(w, "P", P, _F32, (T, R), dev)
+    _check(LIB.gm_lora_bwd(y, ldy, x, ldx, _on(w, "A", A, _BF16, None, dev), _on(w, "B", B, _BF16, None, dev),
+                           _on(w, "scale", scale, _F32, (n,), dev), _on(w, "plan", plan, _U8, None, dev), plan.numel(), p,
+                           T, n, d_in, parts, len(parts), r, b, ldb, dx, lddx, da, db, _on(w, "ws", ws, _U8, None, dev),
+                           ws.numel(), _stream(stream)), w)
 
 
 # ---- the optimiser's work over lists of tensors
@@ -551,8 +567,11 @@ def gm_tensor_list(g, list, p=None, m=None, v=None, p16=None, stream=None) -> No
     for t in g:
         if t.dtype is not torch.float32 and t.dtype is not torch.bfloat16:
             raise ValueError(f"{w}: gradients must be {torch.float32} or {torch.bfloat16}, got {t.dtype}")
-    _arg(w, "list", list, "u8")
-    _one_device(w, list, *g, *(t for ts in rest.values() for t in ts))
+    dev = _device()
+    at = _on(w, "list", list, _U8, None, dev)
+    for t in (*g, *(t for ts in rest.values() for t in ts)):
+        if t.get_device() != dev:
+            raise ValueError(f"{w}: every tensor must live on the current GPU, got one on {t.device}")
 
     def array(ts):
         return None if ts is None else (ctypes.c_void_p * max(n, 1))(*(_ptr(t) if t.numel() else None for t in ts))
@@ -560,27 +579,27 @@ def gm_tensor_list(g, list, p=None, m=None, v=None, p16=None, stream=None) -> No
     numel = (ctypes.c_int64 * max(n, 1))(*(t.numel() for t in g))
     b16 = (ctypes.c_uint8 * max(n, 1))(*(t.dtype is torch.bfloat16 for t in g))
     _check(LIB.gm_tensor_list(array(rest.get("p")), array(g), array(rest.get("m")), array(rest.get("v")),
-                              array(rest.get("p16")), b16, numel, n, _ptr(list), list.numel(), _stream(stream)), w)
+                              array(rest.get("p16")), b16, numel, n, at, list.numel(), _stream(stream)), w)
 
 
 def gm_grad_norm(list, max_norm: float, norm, coef, ws, stream=None) -> None:
     """The norm of all gradients of a list, and the coefficient that clips it to max_norm (both fp32, on the device)."""
     w = "gm_grad_norm"
-    _arg(w, "list", list, "u8")
-    _arg(w, "norm", norm, "f32", numel=1)
-    _arg(w, "coef", coef, "f32", numel=1)
-    _arg(w, "ws", ws, "u8")
-    _one_device(w, list, norm, coef, ws)
-    _check(LIB.gm_grad_norm(_ptr(list), list.numel(), float(max_norm), _ptr(norm), _ptr(coef), _ptr(ws), ws.numel(),
-                            _stream(stream)), w)
+    dev = _device()
+    if norm.numel() != 1 or coef.numel() != 1:
+        raise ValueError(f"{w}: norm and coef must hold one element each")
+    _check(LIB.gm_grad_norm(_on(w, "list", list, _U8, None, dev), list.numel(), float(max_norm),
+                            _on(w, "norm", norm, _F32, None, dev), _on(w, "coef", coef, _F32, None, dev),
+                            _on(w, "ws", ws, _U8, None, dev), ws.numel(), _stream(stream)), w)
 
 
 def gm_adamw_list(list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float, step: int, coef=None,
                   stream=None) -> None:
     """One AdamW step on every tensor of a list with the gradients coef g (coef None: 1)."""
     w = "gm_adamw_list"
-    _arg(w, "list", list, "u8")
-    _arg(w, "coef", coef, "f32", numel=1, optional=True)
-    _one_device(w, list, coef)
-    _check(LIB.gm_adamw_list(_ptr(list), list.numel(), float(lr), float(beta1), float(beta2), float(eps),
-                             float(weight_decay), int(step), _ptr(coef), _stream(stream)), w)
+    dev = _device()
+    if coef is not None and coef.numel() != 1:
+        raise ValueError(f"{w}: coef must hold one element")
+    c = None if coef is None else _on(w, "coef", coef, _F32, None, dev)
+    _check(LIB.gm_adamw_list(_on(w, "list", list, _U8, None, dev), list.numel(), float(lr), float(beta1), float(beta2),
+                             float(eps), float(weight_decay), int(step), c, _stream(stream)), w)
