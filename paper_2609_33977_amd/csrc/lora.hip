@@ -837,7 +837,7 @@ struct LoraGrad {
   int64_t ostride;  // elements per adapter
   int ocols;        // all columns of the tall matrix
   float* part;      // the same, per gradient tile
-  int parts;
+  int parts, chunks;  // chunks: blocks of 16 RT ranks
   int off[kLoraMaxParts], width[kLoraMaxParts], first[kLoraMaxParts + 1];
 };
 
@@ -852,24 +852,24 @@ constexpr int kGradStages = RT == 4 ? 3 : 4;
 // index.  The waves split ranks and columns, never tokens, so no sum crosses a wave.
 // An adapter with one gradient tile is done; others leave partial sums.
 template <int RT, bool DB>
-__device__ __forceinline__ void lora_grad_body(const LoraGrad& a, const LoraPlan& plan, int block, u32x4 (*s_stage)[(8 + 3 * RT) * 64],
+__device__ __forceinline__ void lora_grad_body(const LoraGrad& a, const LoraPlan& plan, int block, u32x4* s_mem,
                                                int* s_tok) {
   constexpr int NS = kGradStages<RT>;
   constexpr int NC = 2 * RT;                  // 16-column fragments per wave: 128 RT / 4 columns
   constexpr int COPIES = 8 + 3 * RT;          // 1 KiB each: 4 rows of 128 columns, or one fragment
   constexpr int PER = (COPIES + 3) / 4;       // per wave
-  const int cbk = block % a.first[a.parts], gi = block / a.first[a.parts];
+  const int chunk = block % a.chunks, cbk = block / a.chunks % a.first[a.parts], gi = block / a.chunks / a.first[a.parts];
   const LoraTile tile = plan.tile(plan.gtiles, gi, 4 + plan.glen);
   if (tile.count == 0) return;
   int part = 0;
   while (part + 1 < a.parts && cbk >= a.first[part + 1]) ++part;
   const int cb = (cbk - a.first[part]) * kLoraGradCols, width = a.width[part];
-  const int rb0 = blockIdx.y * RT;  // first block of 16 ranks within the part
+  const int rb0 = chunk * RT;  // first block of 16 ranks within the part
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, q = lane >> 4;
   const int steps = (tile.count + 31) / 32;
   for (int i = threadIdx.x; i < 32 * steps; i += 256) s_tok[i] = plan.tokens[tile.pos * kLoraTile + i];
   __syncthreads();
-  const uint32_t lds = lds_addr(s_stage);
+  const uint32_t lds = lds_addr(s_mem);
   const uint16_t* x = a.X + a.off[part] + cb;
   const uint16_t* terms = a.terms + (int64_t(tile.pos) * 2 * a.tblocks + part * a.pblocks) * (3 * 512) + lane * 8;
   auto issue = [&](int step) {
@@ -900,7 +900,7 @@ __device__ __forceinline__ void lora_grad_body(const LoraGrad& a, const LoraPlan
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     block_sync();
     if (s + NS - 1 < steps) issue(s + NS - 1);
-    const u32x4* st = s_stage[s % NS];
+    const u32x4* st = s_mem + s % NS * (COPIES * 64);
     u32x4 f[3];
 #pragma unroll
     for (int m = 0; m < 3; ++m) f[m] = st[(8 + 3 * rb + m) * 64 + lane];
@@ -929,15 +929,19 @@ __device__ __forceinline__ void lora_grad_body(const LoraGrad& a, const LoraPlan
   }
 }
 
-// Both gradients in one launch where their ranks go in blocks of the same size: the blocks of dA, then dB's.
+// Slots of 16 bytes that the stages take.
 template <int RT>
+constexpr int kGradSlots = kGradStages<RT> * (8 + 3 * RT) * 64;
+
+// Both gradients in one launch: dA's blocks, over all parts' ranks, then dB's, over one part's.
+template <int RTA, int RTB>
 __global__ __launch_bounds__(256, 2) void lora_grad_kernel(LoraGrad a, int blocksA, LoraGrad b, LoraPlan plan) {
-  __shared__ u32x4 s_stage[kGradStages<RT>][(8 + 3 * RT) * 64];
+  __shared__ u32x4 s_mem[kGradSlots<RTA> > kGradSlots<RTB> ? kGradSlots<RTA> : kGradSlots<RTB>];
   __shared__ int s_tok[kLoraGradMost];
   if (int(blockIdx.x) < blocksA)
-    lora_grad_body<RT, false>(a, plan, blockIdx.x, s_stage, s_tok);
+    lora_grad_body<RTA, false>(a, plan, blockIdx.x, s_mem, s_tok);
   else
-    lora_grad_body<RT, true>(b, plan, blockIdx.x - blocksA, s_stage, s_tok);
+    lora_grad_body<RTB, true>(b, plan, blockIdx.x - blocksA, s_mem, s_tok);
 }
 
 // The gradients of adapters with several tiles from their partial sums, in the
@@ -1037,25 +1041,24 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   return launch_up<false>(u, z.r, tiles, pl, s);
 }
 
-static hipError_t launch_grad(const LoraGrad& a, const LoraGrad& b, int ranks, const LoraPlan& plan, int gtiles,
-                              hipStream_t s) {
-  const int rt = rank_tiles(ranks), blocksA = gtiles * a.first[a.parts], blocksB = gtiles * b.first[b.parts];
-  const dim3 grid(unsigned(blocksA) + unsigned(blocksB), unsigned((ranks + 16 * rt - 1) / (16 * rt))), block(256);
-  switch (rt) {
-    case 1: hipLaunchKernelGGL(lora_grad_kernel<1>, grid, block, 0, s, a, blocksA, b, plan); break;
-    case 2: hipLaunchKernelGGL(lora_grad_kernel<2>, grid, block, 0, s, a, blocksA, b, plan); break;
-    default: hipLaunchKernelGGL(lora_grad_kernel<4>, grid, block, 0, s, a, blocksA, b, plan); break;
-  }
+static hipError_t launch_grad(LoraGrad& a, LoraGrad& b, const LoraPlan& plan, int gtiles, hipStream_t s) {
+  const int ra = rank_tiles(a.r), rb = rank_tiles(b.r);
+  a.chunks = (a.r + 16 * ra - 1) / (16 * ra), b.chunks = (b.r + 16 * rb - 1) / (16 * rb);
+  const int blocksA = gtiles * a.first[a.parts] * a.chunks, blocksB = gtiles * b.first[b.parts] * b.chunks;
+  const dim3 grid(unsigned(blocksA) + unsigned(blocksB)), block(256);
+  // dA has at least as many ranks as dB
+  if (ra == 1) hipLaunchKernelGGL((lora_grad_kernel<1, 1>), grid, block, 0, s, a, blocksA, b, plan);
+  else if (ra == 2 && rb == 1) hipLaunchKernelGGL((lora_grad_kernel<2, 1>), grid, block, 0, s, a, blocksA, b, plan);
+  else if (ra == 2) hipLaunchKernelGGL((lora_grad_kernel<2, 2>), grid, block, 0, s, a, blocksA, b, plan);
+  else if (rb == 1) hipLaunchKernelGGL((lora_grad_kernel<4, 1>), grid, block, 0, s, a, blocksA, b, plan);
+  else if (rb == 2) hipLaunchKernelGGL((lora_grad_kernel<4, 2>), grid, block, 0, s, a, blocksA, b, plan);
+  else hipLaunchKernelGGL((lora_grad_kernel<4, 4>), grid, block, 0, s, a, blocksA, b, plan);
   return hipGetLastError();
 }
 
 int lora_bwd_glen(const LoraShape& z) {
   int64_t blocks = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
   for (int p = 0; p < z.parts; ++p) blocks += (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
-  if (z.parts > 1) {  // two launches
-    const int64_t a = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
-    blocks = a < blocks - a ? a : blocks - a;
-  }
   return lora_grad_len(z.T, blocks);
 }
 
@@ -1095,15 +1098,16 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
     u.Qn = w.Qn, u.blocksQ = m.blocksQ, u.parts = 1, u.width[0] = z.d_in;
     if ((e = launch_up<true>(u, R, tiles, pl, s))) return e;
   }
-  LoraGrad ga = {}, gb = {}, none = {};
+  LoraGrad ga = {}, gb = {};
+  ga.r = R, gb.r = z.r;
   if (dA) {
-    ga.X = X, ga.ldx = ldx, ga.terms = w.Qt, ga.tblocks = ga.pblocks = m.blocksQ, ga.r = R;
+    ga.X = X, ga.ldx = ldx, ga.terms = w.Qt, ga.tblocks = ga.pblocks = m.blocksQ;
     ga.out = dA, ga.ostride = int64_t(R) * z.d_in, ga.ocols = z.d_in, ga.part = w.partA, ga.parts = 1;
     ga.width[0] = z.d_in;
     ga.first[1] = (z.d_in + kLoraGradCols - 1) / kLoraGradCols;
   }
   if (dB) {
-    gb.X = dY, gb.ldx = lddy, gb.terms = w.Pt, gb.tblocks = m.blocksP, gb.pblocks = m.blocksP / z.parts, gb.r = z.r;
+    gb.X = dY, gb.ldx = lddy, gb.terms = w.Pt, gb.tblocks = m.blocksP, gb.pblocks = m.blocksP / z.parts;
     gb.scale = scale, gb.out = dB, gb.ostride = int64_t(z.d_out) * z.r, gb.ocols = z.d_out, gb.part = w.partB;
     gb.parts = z.parts;
     for (int p = 0; p < z.parts; ++p) {
@@ -1111,12 +1115,7 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
       gb.first[p + 1] = gb.first[p] + (z.widths[p] + kLoraGradCols - 1) / kLoraGradCols;
     }
   }
-  if (z.parts == 1 && (dA || dB)) {
-    if ((e = launch_grad(ga, gb, R, pl, gtiles, s))) return e;
-  } else {
-    if (dA && (e = launch_grad(ga, none, R, pl, gtiles, s))) return e;
-    if (dB && (e = launch_grad(none, gb, z.r, pl, gtiles, s))) return e;
-  }
+  if ((dA || dB) && (e = launch_grad(ga, gb, pl, gtiles, s))) return e;
   if (dA || dB) {
     const int64_t sA = int64_t(R) * z.d_in, sB = int64_t(z.d_out) * z.r;
     const unsigned bA = dA ? unsigned((sA + 1023) / 1024) : 0, bB = dB ? unsigned((sB + 1023) / 1024) : 0;
