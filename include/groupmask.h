@@ -403,10 +403,11 @@ gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64_t n, doub
  * significand; in dA and dB with all 24); Y and dX are rounded once.  Values
  * of a token or of its adapter that are not finite make its rows (and that
  * adapter's gradients) not finite, and no others.  Results do not
- * depend on timing, and a token's Y and P not on the order of the batch.
+ * depend on timing; the order of the batch changes the order of fp32 sums only.
  *   1 <= T <= 262144; 1 <= n <= 2048; r a multiple of 8 in [8, 128];
  *   1 <= parts <= 4; d_in and every width multiples of 8, d_in and d_out at
- *   most 2^18.  widths is a HOST array.  X, dY, base, Y and dX have a row
+ *   most 2^18 each, and (T + 63 min(n + 1, T)) / 64 (d_in + d_out) at most 2^30.
+ *   widths is a HOST array.  X, dY, base, Y and dX have a row
  *   stride in elements (ldx ...), a multiple of 8 and at least the row's length,
  *   so that they may be columns of wider buffers; base may be Y (dX) itself
  *   with the same stride, else it must not overlap it.  All but `adapter`
@@ -458,8 +459,9 @@ gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64
  * NULL parameters p[i] with moments m[i] and v[i], all fp32, and unless p16 is NULL a bf16 copy
  * p16[i] of the parameters.  g[i] is bf16 where g_bf16 (may be NULL) is not 0, else fp32.
  * All these arrays are HOST arrays (read before the call returns) of DEVICE
- * pointers, which need their element's alignment only; tensors that are
- * all 16-byte aligned (p16: 8) go faster.  The list holds the addresses, not
+ * pointers, which need their element's alignment only; the step goes
+ * faster where a tensor's buffers lie alike to 16 bytes (p16: 8), as those do that
+ * are aligned to 16 bytes or cut alike from one buffer per role.  The list holds the addresses, not
  * the values: it stays good while the buffers live, and the calls below that
  * take it need it ordered before them on their stream.
  *   1 <= n <= 65536; numel[i] >= 0 (pointers of empty tensors may be NULL).

@@ -279,6 +279,7 @@ constexpr int64_t kMaxLoraTokens = 262144;
 constexpr int32_t kMaxAdapters = 2048;
 constexpr int64_t kMaxLoraDim = int64_t(1) << 18;
 constexpr int32_t kMaxRank = 128;
+constexpr int64_t kMaxLoraTileColumns = int64_t(1) << 30;  // 64-token tiles times d_in + d_out
 
 gm_status check_lora_batch(int64_t T, int32_t n) {
   return T < 1 || T > kMaxLoraTokens || n < 1 || n > kMaxAdapters ? GM_ERR_SHAPE : GM_OK;
@@ -299,6 +300,8 @@ gm_status check_lora_shape(int64_t T, int32_t n, int64_t d_in, const int64_t* wi
     d_out += widths[p];
   }
   if (d_out > kMaxLoraDim) return GM_ERR_SHAPE;
+  // a launch has fewer than 2^32 threads
+  if (gm::lora_plan_layout(T, n).max_tiles * (d_in + d_out) > kMaxLoraTileColumns) return GM_ERR_SHAPE;
   z->d_out = int(d_out);
   return GM_OK;
 }

@@ -146,6 +146,14 @@ def test_backward_refusals():
     assert _bwd(dX=None, dA=None, dB=None, P=None, base=None, ws=None) == gm.GM_OK   # nothing asked for
 
 
+def test_launch_limit():
+    # (T + 63 min(n + 1, T)) / 64 tiles times d_in + d_out up to 2^30
+    assert gm.gm_lora_workspace_size(gm.GM_OP_FWD, 262144 - 126, 1, 1 << 17, 1 << 17, 8) > 0
+    out = ctypes.c_size_t(0)
+    assert gm.LIB.gm_lora_workspace_size(gm.GM_OP_FWD, 262144, 1, 1 << 17, _widths(1 << 17), 1, 8,
+                                         ctypes.byref(out)) == gm.GM_ERR_SHAPE
+
+
 def test_workspace_op_and_null():
     out = ctypes.c_size_t(0)
     assert gm.LIB.gm_lora_workspace_size(5, 10, 2, 64, _widths(64), 1, 16, ctypes.byref(out)) == gm.GM_ERR_VALUE
