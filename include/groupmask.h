@@ -410,7 +410,7 @@ gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64_t n, doub
  *   widths is a HOST array.  X, dY, base, Y and dX have a row
  *   stride in elements (ldx ...), a multiple of 8 and at least the row's length,
  *   so that they may be columns of wider buffers; base may be Y (dX) itself
- *   with the same stride, else it must not overlap it.  All but `adapter`
+ *   with the same stride, else no output may overlap an input.  All but `adapter`
  *   (4-byte aligned) and scale are 16-byte aligned.
  *
  * gm_lora_plan_size, gm_lora_workspace_size (op GM_OP_FWD or GM_OP_BWD) --
@@ -464,7 +464,9 @@ gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64
  * are aligned to 16 bytes or cut alike from one buffer per role.  The list holds the addresses, not
  * the values: it stays good while the buffers live, and the calls below that
  * take it need it ordered before them on their stream.
- *   1 <= n <= 65536; numel[i] >= 0 (pointers of empty tensors may be NULL).
+ *   1 <= n <= 65536; numel[i] >= 0 (pointers of empty tensors may be NULL).  No
+ *   buffer that a step writes may share memory with another buffer of the list
+ *   (GM_ERR_VALUE; a parameter twice, say); gradients may share theirs, and count as often.
  */
 gm_status gm_tensor_list_size(const int64_t* numel, int32_t n, size_t* bytes);
 gm_status gm_tensor_list(float* const* p, const void* const* g, float* const* m, float* const* v,

@@ -8,7 +8,9 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <memory>
 #include <mutex>
+#include <new>
 
 #include "../../include/groupmask.h"
 #include "gm_launch.h"
@@ -769,6 +771,40 @@ gm_status list_size(const int64_t* numel, int32_t n, size_t* bytes) {
   return GM_OK;
 }
 
+struct ListSpan {
+  uintptr_t begin, end;
+  bool written;
+};
+
+// Whether a buffer that the step writes (p, m, v, p16) shares bytes with another buffer of the list: blocks
+// would race for them.  Gradients may share theirs.
+gm_status list_overlap(float* const* p, const void* const* g, float* const* m, float* const* v,
+                       uint16_t* const* p16, const uint8_t* g_bf16, const int64_t* numel, int32_t n) {
+  if (!p) return GM_OK;
+  const size_t count = size_t(n) * 5;
+  std::unique_ptr<ListSpan[]> spans(new (std::nothrow) ListSpan[count]);
+  if (!spans) return GM_ERR_WORKSPACE;
+  size_t k = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (numel[i] == 0) continue;
+    auto take = [&](const void* x, int64_t size, bool written) {
+      const uintptr_t b = reinterpret_cast<uintptr_t>(x);
+      spans[k++] = {b, b + uintptr_t(numel[i] * size), written};
+    };
+    take(p[i], 4, true), take(m[i], 4, true), take(v[i], 4, true);
+    if (p16) take(p16[i], 2, true);
+    take(g[i], g_bf16 && g_bf16[i] ? 2 : 4, false);
+  }
+  std::sort(spans.get(), spans.get() + k, [](const ListSpan& a, const ListSpan& b) { return a.begin < b.begin; });
+  uintptr_t any = 0, written = 0;  // ends of what came before
+  for (size_t i = 0; i < k; ++i) {
+    if (spans[i].begin < written || (spans[i].written && spans[i].begin < any)) return GM_ERR_VALUE;
+    any = std::max(any, spans[i].end);
+    if (spans[i].written) written = std::max(written, spans[i].end);
+  }
+  return GM_OK;
+}
+
 }  // namespace
 
 GM_EXPORT gm_status gm_tensor_list_size(const int64_t* numel, int32_t n, size_t* bytes) {
@@ -793,6 +829,7 @@ GM_EXPORT gm_status gm_tensor_list(float* const* p, const void* const* g, float*
   }
   if (!aligned16(list)) return GM_ERR_ALIGN;
   if (list_bytes < need) return GM_ERR_WORKSPACE;
+  if (gm_status st = list_overlap(p, g, m, v, p16, g_bf16, numel, n)) return st;
   if (gm_status st = check_device()) return st;
   return from_hip(gm::launch_tensor_list(p, g, m, v, p16, g_bf16, numel, n, list, stream));
 }

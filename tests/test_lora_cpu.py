@@ -190,8 +190,8 @@ def test_binding_refuses_before_the_library():
 
 def _list_args(sizes, **change):
     n = len(sizes)
-    ptrs = lambda v=1 << 20: (ctypes.c_void_p * max(n, 1))(*[v] * n)  # noqa: E731
-    a = dict(p=ptrs(), g=ptrs(), m=ptrs(), v=ptrs(), p16=ptrs(), b16=None, numel=(ctypes.c_int64 * max(n, 1))(*sizes), n=n,
+    ptrs = lambda role: (ctypes.c_void_p * max(n, 1))(*[(role * 64 + i + 1) << 20 for i in range(n)])  # noqa: E731
+    a = dict(p=ptrs(0), g=ptrs(1), m=ptrs(2), v=ptrs(3), p16=ptrs(4), b16=None, numel=(ctypes.c_int64 * max(n, 1))(*sizes), n=n,
              list=FAKE, bytes=BIG, stream=None)
     return tuple((a | change).values())
 
@@ -216,6 +216,21 @@ def test_list_refusals():
     assert f(*_list_args([1 << 40] * 9)) == gm.GM_ERR_SHAPE                      # more chunks than an int counts
     assert f(*_list_args([5], list=ODD)) == gm.GM_ERR_ALIGN
     assert f(*_list_args([5], bytes=gm.gm_tensor_list_size([5]) - 1)) == gm.GM_ERR_WORKSPACE
+
+
+def test_list_refuses_shared_memory():
+    # fake addresses: GM_ERR_DEVICE (no GPU here, or nothing launched there) would mean that the list was accepted
+    f = gm.LIB.gm_tensor_list
+    ptr = lambda *v: (ctypes.c_void_p * len(v))(*v)  # noqa: E731
+    a = 1 << 30
+    for name in ("p", "m", "v"):
+        for second in (a, a + 4 * 99):                                           # the same buffer, or its last value
+            assert f(*_list_args([100, 100], **{name: ptr(a, second)})) == gm.GM_ERR_VALUE
+    assert f(*_list_args([100, 100], p16=ptr(a, a + 2 * 99))) == gm.GM_ERR_VALUE
+    assert f(*_list_args([100], p=ptr(a), g=ptr(a))) == gm.GM_ERR_VALUE          # a gradient that is its parameter
+    assert f(*_list_args([100], m=ptr(a), v=ptr(a + 200))) == gm.GM_ERR_VALUE
+    big = _list_args([10, 1000, 10], g=ptr(1 << 40, a, a + 40), p=ptr(1 << 41, 1 << 42, a + 3996))
+    assert f(*big) == gm.GM_ERR_VALUE                                            # inside a long gradient that began before
 
 
 def test_norm_and_step_refusals():
