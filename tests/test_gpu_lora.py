@@ -31,6 +31,7 @@ SIZES = [  # T, n, d_in, widths, r, routing
     (257, 1, 128, (256,), 72, "all"), (300, 5, 640, (40, 40, 40, 40), 128, "bad"), (513, 2, 72, (1032,), 16, "runs"),
     (600, 2048, 64, (32,), 8, "mixed"), (1000, 7, 264, (200, 56), 56, "bad"), (4100, 3, 40, (24,), 8, "runs"),
     (5000, 1, 136, (264,), 16, "all"), (12, 2, 24, (16,), 8, "none"),
+    (20000, 1024, 16, (8,), 8, "mixed"), (9000, 1025, 8, (24,), 8, "bad"),
 ]
 
 

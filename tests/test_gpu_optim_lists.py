@@ -147,6 +147,15 @@ def test_only_gradients_and_repeats():
     torch.cuda.synchronize()
 
 
+def test_a_gradient_twice_counts_twice():
+    import paper_2609_33977_amd as gm
+    g, *_ = _make([9001])
+    norm, _ = _norm(gm, _list(gm, [g[0], g[0], g[0][1:]]), 1.0)
+    h = _h([g[0], g[0], g[0][1:]])
+    want = oracle.grad_norm(h, 1.0)[0]
+    assert abs(float(norm) - want) <= 2.0 ** -23 * want
+
+
 def test_something_that_is_no_list_is_not_followed():
     import paper_2609_33977_amd as gm
     import torch
