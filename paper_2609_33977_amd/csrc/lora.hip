@@ -62,9 +62,11 @@ static LoraPlan lora_plan(const void* plan, int T, int n, int glen) {
           reinterpret_cast<const LoraTile*>(w + L.gtiles[glen]), w + L.gstart[glen], glen, T, n};
 }
 
-// Lanes of the wave with the same key, as a mask.
+// Lanes of the wave with the same key, as a mask; runs of one key are told at once.
 __device__ __forceinline__ uint64_t same_key(int key, int bits, bool on) {
   uint64_t m = __ballot(on);
+  if ((__ballot(key != __builtin_amdgcn_readfirstlane(key)) & m) == 0) return m;
+#pragma unroll 1
   for (int b = 0; b < bits; ++b) {
     const uint64_t one = __ballot((key >> b) & 1);
     m &= (key >> b) & 1 ? one : ~one;
