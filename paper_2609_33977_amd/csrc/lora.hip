@@ -446,12 +446,12 @@ __global__ __launch_bounds__(256, 2) void lora_down_kernel(LoraDown a, LoraPlan 
 // Sum of the splits' partial sums at p, four values.
 __device__ __forceinline__ f32x4 sum_splits(const float* p, int splits, int64_t stride) {
   f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < splits; s += 8) {
-    f32x4 u[8];
+  for (int s = 0; s < splits; s += 4) {
+    f32x4 u[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4*>(p + min(s + i, splits - 1) * stride);
+    for (int i = 0; i < 4; ++i) u[i] = *reinterpret_cast<const f32x4*>(p + min(s + i, splits - 1) * stride);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
       if (s + i < splits) v += u[i];
   }
   return v;
@@ -808,7 +808,7 @@ __device__ __forceinline__ void lora_up_body(const LoraUp& a, const LoraPlan& pl
 }
 
 template <int RT, bool TR, bool MULTI>
-__global__ __launch_bounds__(256, RT == 8 && !TR ? 1 : 2) void lora_up_kernel(LoraUp a, LoraPlan plan) {
+__global__ __launch_bounds__(256, RT == 8 && !TR ? 1 : RT == 1 ? 6 : 2) void lora_up_kernel(LoraUp a, LoraPlan plan) {
   __shared__ u32x4 s_w[kUpCols<RT> * 2 * RT];
   __shared__ __align__(16) uint16_t s_terms[TR ? 8 : 64 * kUpPitch<RT>];
   const int blocks = a.first[a.parts], ti = blockIdx.x / blocks, cbk = blockIdx.x % blocks;
