@@ -406,7 +406,7 @@ gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64_t n, doub
  * depend on timing; the order of the batch changes the order of fp32 sums only.
  *   1 <= T <= 262144; 1 <= n <= 2048; r a multiple of 8 in [8, 128];
  *   1 <= parts <= 4; d_in and every width multiples of 8, d_in and d_out at
- *   most 2^18 each, and (T + 63 min(n + 1, T)) / 64 (d_in + d_out) at most 2^30.
+ *   most 2^18 each, and (T + 63 min(n + 1, T)) / 64 (d_in + d_out) at most 2^27.
  *   widths is a HOST array.  X, dY, base, Y and dX have a row
  *   stride in elements (ldx ...), a multiple of 8 and at least the row's length,
  *   so that they may be columns of wider buffers; base may be Y (dX) itself

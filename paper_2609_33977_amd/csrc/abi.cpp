@@ -281,7 +281,7 @@ constexpr int64_t kMaxLoraTokens = 262144;
 constexpr int32_t kMaxAdapters = 2048;
 constexpr int64_t kMaxLoraDim = int64_t(1) << 18;
 constexpr int32_t kMaxRank = 128;
-constexpr int64_t kMaxLoraTileColumns = int64_t(1) << 30;  // 64-token tiles times d_in + d_out
+constexpr int64_t kMaxLoraTileColumns = int64_t(1) << 27;  // 64-token tiles times d_in + d_out
 
 gm_status check_lora_batch(int64_t T, int32_t n) {
   return T < 1 || T > kMaxLoraTokens || n < 1 || n > kMaxAdapters ? GM_ERR_SHAPE : GM_OK;

@@ -147,10 +147,10 @@ def test_backward_refusals():
 
 
 def test_launch_limit():
-    # (T + 63 min(n + 1, T)) / 64 tiles times d_in + d_out up to 2^30
-    assert gm.gm_lora_workspace_size(gm.GM_OP_FWD, 262144 - 126, 1, 1 << 17, 1 << 17, 8) > 0
+    # (T + 63 min(n + 1, T)) / 64 tiles times d_in + d_out up to 2^27
+    assert gm.gm_lora_workspace_size(gm.GM_OP_FWD, 262144 - 126, 1, 1 << 14, 1 << 14, 8) > 0
     out = ctypes.c_size_t(0)
-    assert gm.LIB.gm_lora_workspace_size(gm.GM_OP_FWD, 262144, 1, 1 << 17, _widths(1 << 17), 1, 8,
+    assert gm.LIB.gm_lora_workspace_size(gm.GM_OP_FWD, 262144, 1, 1 << 14, _widths(1 << 14), 1, 8,
                                          ctypes.byref(out)) == gm.GM_ERR_SHAPE
 
 
