@@ -1021,17 +1021,29 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
 // Blocks of 16, 32 or 64 ranks.
 static int rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
 
-// Blocks of up to 1024 columns, down to 256 where there are few tiles: four blocks per CU to hide latency (4099
-// tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
-// terms that every block stages count for more: high ranks (8192 tokens, 4096 columns, 64 ranks: 36 with two, 43 with
-// four) and tiles of few tokens (64 tokens of 32 adapters, 15360 columns, 16 ranks: 9.0 and 11.4).
+// Blocks of 1024 to 256 columns.  Up to 32 ranks, and for dX, narrower ones until there are four blocks per CU to hide
+// latency (4099 tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
+// terms that every block stages count for more, in tiles of few tokens (64 tokens of 32 adapters, 15360
+// columns: 9.0 us with two, 11.4 with four).  Beyond, where 768 blocks fit the chip at once and staging costs a block
+// about as much as 384 columns, the width whose rounds of blocks cost least: 8192 tokens of one
+// adapter, 4096 columns, 64 ranks, one round of 1024 columns 36 us, two of 512 43; 203 tokens of 40 adapters,
+// 22016 columns, two rounds of 1024 33, three of 512 29.
 template <bool TR>
 static int up_blocks(LoraUp& u, int ranks, int tiles, const LoraPlan& plan) {
-  int cols = 0;
-  for (int p = 0; p < u.parts; ++p) cols += u.width[p];
-  const int want = TR || (ranks <= 32 && plan.T >= tiles * (kLoraTile / 2)) ? 1024 : 512;
+  auto blocks = [&](int span) {
+    int64_t n = 0;
+    for (int p = 0; p < u.parts; ++p) n += (u.width[p] + span - 1) / span;
+    return n * tiles;
+  };
   u.span = 1024;
-  while (u.span > 256 && int64_t(tiles) * (cols / u.span) < want) u.span /= 2;
+  if (TR || ranks <= 32) {
+    const int want = TR || plan.T >= tiles * (kLoraTile / 2) ? 1024 : 512;
+    while (u.span > 256 && blocks(u.span) < want) u.span /= 2;
+  } else {
+    auto cost = [&](int span) { return (blocks(span) + 767) / 768 * (span + 384); };
+    for (int span = 512; span >= 256; span /= 2)
+      if (cost(span) < cost(u.span)) u.span = span;
+  }
   if (ranks > 128) u.span = kUpCols<8>;
   for (int p = 0, off = 0; p < u.parts; ++p) {
     u.off[p] = off;
