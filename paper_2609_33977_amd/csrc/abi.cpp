@@ -312,12 +312,12 @@ gm_status check_lora_shape(int64_t T, int32_t n, int64_t d_in, const int64_t* wi
 bool lora_rows_ok(int64_t ld, int64_t cols) { return ld >= cols && ld % 8 == 0 && ld <= (int64_t(1) << 32); }
 
 int lora_fwd_splits(const gm::LoraShape& z) {
-  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles, z.d_in);
+  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles, z.parts * z.r, z.d_in);
 }
 int lora_bwd_splits(const gm::LoraShape& z) {
   int widest = 0;
   for (int p = 0; p < z.parts; ++p) widest = std::max(widest, z.widths[p]);
-  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles * z.parts, widest);
+  return gm::lora_splits(gm::lora_plan_layout(z.T, z.n).max_tiles * z.parts, z.r, widest);
 }
 
 // Workspace of the adapters' backward, each part 256-byte aligned (see gm::LoraBwdWs).

@@ -64,12 +64,17 @@ inline int lora_grad_len(int64_t T, int64_t col_blocks) {
   return i;
 }
 
-// Blocks that share a tile's contraction over K: enough to fill the chip with
-// `tiles` tiles, at least one slice each, and few enough that their partial
-// sums stay small beside the operand.
-inline int lora_splits(int64_t tiles, int64_t K) {
-  const int64_t slices = (K + kLoraSlice - 1) / kLoraSlice;
-  int64_t ks = 512 / (tiles < 512 ? tiles : 512);
+// Blocks of 16, 32 or 64 ranks.
+inline int lora_rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
+
+// Blocks that share a tile's contraction over K: two blocks per CU (what fits at once at 64 ranks; a
+// sixteenth more, since the tiles are the most that there can be), at least two and at most one per slice.  8192
+// tokens of 11008 columns, 64 ranks: 51 us with three splits of 128 tiles, 48 with four.  Three blocks per CU, which fit at
+// fewer ranks, gave nothing there (4099 tokens of 4096 columns, 16 ranks: 9.6 and 10.2 us).
+inline int lora_splits(int64_t tiles, int ranks, int64_t K) {
+  const int rt = lora_rank_tiles(ranks);
+  const int64_t slices = (K + kLoraSlice - 1) / kLoraSlice, chunks = (ranks + 16 * rt - 1) / (16 * rt);
+  int64_t ks = 544 / (tiles * chunks);
   if (ks < 2) ks = 2;
   return int(ks < slices ? ks : slices);
 }

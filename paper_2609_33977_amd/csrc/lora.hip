@@ -1018,9 +1018,6 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
   return hipGetLastError();
 }
 
-// Blocks of 16, 32 or 64 ranks.
-static int rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
-
 // Blocks of 1024 to 256 columns.  Up to 32 ranks, and for dX, narrower ones until there are four blocks per CU to hide
 // latency (4099 tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
 // terms that every block stages count for more, in tiles of few tokens (64 tokens of 32 adapters, 15360
@@ -1073,7 +1070,7 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
   d.X = X, d.ldx = ldx, d.W = A, d.wstride = int64_t(R) * z.d_in, d.K = z.d_in, d.wrows = R;
   d.part = part, d.R = R;
   d.splits = splits;
-  const int rt = rank_tiles(R);
+  const int rt = lora_rank_tiles(R);
   d.chunks = (R + 16 * rt - 1) / (16 * rt);
   if (hipError_t e = launch_down<false>(d, pl, tiles, rt, d.chunks, s)) return e;
   LoraUp u = {};
@@ -1088,7 +1085,7 @@ hipError_t launch_lora_fwd(const uint16_t* X, int64_t ldx, const uint16_t* A, co
 // The gradients that are asked for, and dX (unless u is null) in the same launch.
 static hipError_t launch_grad(LoraGrad& a, LoraGrad& b, LoraUp* u, int tiles, const LoraPlan& plan, int gtiles,
                               hipStream_t s) {
-  const int ra = rank_tiles(a.r), rb = rank_tiles(b.r);
+  const int ra = lora_rank_tiles(a.r), rb = lora_rank_tiles(b.r);
   a.chunks = (a.r + 16 * ra - 1) / (16 * ra), b.chunks = (b.r + 16 * rb - 1) / (16 * rb);
   const int blocksA = gtiles * a.first[a.parts] * a.chunks, blocksB = gtiles * b.first[b.parts] * b.chunks;
   const int blocksU = u ? up_blocks<true>(*u, a.r, tiles, plan) : 0;
@@ -1135,7 +1132,7 @@ hipError_t launch_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, 
     d.X = dY, d.ldx = lddy, d.W = B, d.wstride = int64_t(z.d_out) * z.r, d.K = widest, d.wrows = z.r;
     d.part = w.part, d.R = R, d.splits = splits;
     for (int p = 0; p < z.parts; ++p) d.off[p] = off[p], d.width[p] = z.widths[p];
-    const int rt = rank_tiles(z.r);
+    const int rt = lora_rank_tiles(z.r);
     d.chunks = (z.r + 16 * rt - 1) / (16 * rt);
     if ((e = launch_down<true>(d, pl, tiles, rt, d.chunks * z.parts, s))) return e;
   }
