@@ -487,7 +487,8 @@ gm_status gm_grad_norm(const void* list, size_t list_bytes, float max_norm, floa
  * gm_adamw_list -- one gm_adamw step on every tensor of the list with the gradients coef g
  * (coef: one fp32 (device), or NULL for 1), and the bf16 copies of the new
  * parameters.  The gradients themselves stay as they are.  With coef = 0, as
- * gm_grad_norm gives it for gradients that are not finite, nothing is changed.
+ * gm_grad_norm gives it for gradients that are not finite (or any coef that is
+ * not positive and finite), nothing is changed.
  * A list without parameters is a no-op.
  */
 gm_status gm_adamw_list(const void* list, size_t list_bytes, double lr, double beta1, double beta2, double eps,

@@ -472,8 +472,8 @@ def gm_lora_workspace_size(op: int, T: int, n: int, d_in: int, widths, r: int) -
 def gm_lora_plan(adapter, n: int, plan, stream=None) -> None:
     """Sorts the tokens of a batch by adapter (see gm_lora_plan in the header); adapter [T] int32."""
     w = "gm_lora_plan"
-    if adapter.dim() != 1:
-        raise ValueError(f"{w}: adapter must have shape (T,), got {tuple(adapter.shape)}")
+    if adapter is None or adapter.dim() != 1:
+        raise ValueError(f"{w}: adapter must have shape (T,), got {None if adapter is None else tuple(adapter.shape)}")
     dev = _device()
     a, p = _on(w, "adapter", adapter, torch.int32, None, dev), _on(w, "plan", plan, _U8, None, dev)
     _check(LIB.gm_lora_plan(a, adapter.shape[0], int(n), p, plan.numel(), _stream(stream)), w)
@@ -481,6 +481,8 @@ def gm_lora_plan(adapter, n: int, plan, stream=None) -> None:
 
 def _adapters(w, X, A, B, widths):
     """(T, n, R, d_in, d_out, r, C array of widths) of tokens and a pool, whose dtypes are checked with their pointers."""
+    if X is None or A is None or B is None:
+        raise ValueError(f"{w}: X, A and B are required")
     if X.dim() != 2 or A.dim() != 3 or B.dim() != 3:
         raise ValueError(f"{w}: X must be [T, d_in], A [n, ranks, d_in] and B [n, d_out, r], got {tuple(X.shape)}, "
                          f"{tuple(A.shape)} and {tuple(B.shape)}")
@@ -586,10 +588,10 @@ def gm_grad_norm(list, max_norm: float, norm, coef, ws, stream=None) -> None:
     """The norm of all gradients of a list, and the coefficient that clips it to max_norm (both fp32, on the device)."""
     w = "gm_grad_norm"
     dev = _device()
+    n, c = _on(w, "norm", norm, _F32, None, dev), _on(w, "coef", coef, _F32, None, dev)
     if norm.numel() != 1 or coef.numel() != 1:
         raise ValueError(f"{w}: norm and coef must hold one element each")
-    _check(LIB.gm_grad_norm(_on(w, "list", list, _U8, None, dev), list.numel(), float(max_norm),
-                            _on(w, "norm", norm, _F32, None, dev), _on(w, "coef", coef, _F32, None, dev),
+    _check(LIB.gm_grad_norm(_on(w, "list", list, _U8, None, dev), list.numel(), float(max_norm), n, c,
                             _on(w, "ws", ws, _U8, None, dev), ws.numel(), _stream(stream)), w)
 
 

@@ -233,9 +233,9 @@ hipError_t launch_tensor_list(float* const* p, const void* const* g, float* cons
       // Values before the gradient's first 16-byte boundary, and whether the step's vectors of four fit the other
       // addresses there too (tensors cut alike from one buffer per role have them in the same place).
       const uintptr_t size = b16 ? 2 : 4, head = ((16 - reinterpret_cast<uintptr_t>(e.g)) & 15) / size;
-      const bool vec = aligned(e.p + head, 16) && aligned(e.m + head, 16) && aligned(e.v + head, 16) &&
+      const bool vec = e.p && aligned(e.p + head, 16) && aligned(e.m + head, 16) && aligned(e.v + head, 16) &&
                        (!e.p16 || aligned(e.p16 + head, 8));
-      e.flags = (b16 ? kListGradBf16 : 0) | (e.p && vec ? kListVector : 0) | int(head) << kListHeadShift;
+      e.flags = (b16 ? kListGradBf16 : 0) | (vec ? kListVector : 0) | int(head) << kListHeadShift;
       w.index[i] = t;
       w.chunks[i] = int(list_chunks(numel[t]));
       first += w.chunks[i];

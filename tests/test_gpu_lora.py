@@ -41,6 +41,11 @@ def test_parity(T, n, d_in, widths, r, kind):
     _both(make(T, n, d_in, widths, r, kind))
 
 
+def test_the_largest_batch():
+    say("adapters: 262144 tokens of 2048 adapters")
+    _both(make(262144, 2048, 8, (8,), 8, "mixed"))
+
+
 def test_llama2_7b_projections():
     say("adapters: T=96, q|k|v 4096 -> 3 x 4096, r=16; T=70, 11008 -> 4096, r=64")
     _both(make(96, 6, 4096, (4096, 4096, 4096), 16, "mixed"))
