@@ -434,7 +434,8 @@ __global__ __launch_bounds__(256, 2) void lora_down_kernel(LoraDown a, LoraPlan 
   const int r0 = chunk * 16 * RT, nr = min(16 * RT, a.wrows - r0);
   const int col0 = BMAJOR ? a.off[part] : 0, K = BMAJOR ? a.width[part] : a.K;
   float* out = a.part + (int64_t(split) * plan.T + tile.pos) * a.R + part * a.wrows + r0;
-  if (split * kLoraSlice >= K) {  // a narrower part than the widest has no slice for this split
+  // A narrower part than the widest may have nothing for this split: tiles of few tokens deal it in slices, others in stages.
+  if (split * (tile.count <= 16 ? kLoraSlice : kDownK) >= K) {
     for (int e = threadIdx.x; e < tile.count * nr; e += 256) out[int64_t(e / nr) * a.R + e % nr] = 0.0f;
   } else if (tile.count <= 16) {
     lora_down_few<RT, BMAJOR>(a, tile, tok, split, K, col0, r0, nr, out, s_mem);

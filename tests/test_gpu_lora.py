@@ -41,6 +41,14 @@ def test_parity(T, n, d_in, widths, r, kind):
     _both(make(T, n, d_in, widths, r, kind))
 
 
+@pytest.mark.parametrize("widths", [(584, 112, 176, 144), (520, 128, 136), (2048, 256, 512, 264), (8, 1100 * 8)])
+@pytest.mark.parametrize("r", [16, 32, 64])
+def test_parts_much_narrower_than_the_widest(widths, r):
+    # 70 tokens of one adapter: a tile of 64 and one of 6, whose narrow parts leave some of the contraction's splits empty
+    say(f"adapters: T=70, widths={widths}, r={r}")
+    _both(make(70, 1, 64, widths, r, "all"))
+
+
 def test_the_largest_batch():
     say("adapters: 262144 tokens of 2048 adapters")
     _both(make(262144, 2048, 8, (8,), 8, "mixed"))
