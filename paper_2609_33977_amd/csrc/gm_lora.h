@@ -56,7 +56,10 @@ inline LoraPlanLayout lora_plan_layout(int64_t T, int64_t n) {
 
 // Which length the gradients of T tokens take: the longest with enough blocks
 // of 128 columns (`col_blocks` for all tokens once) to fill the chip, since every
-// tile of an adapter beyond the first leaves partial sums to be written and added.
+// tile of an adapter beyond the first leaves partial sums to be written and added.  Gradients (with dX) and the adding, us,
+// with tiles of 256 / 512 / 1024 / 2048 tokens: one adapter, 8192 tokens, 4096 and 11008 columns, 64 ranks 131 + 21,
+// 114 + 11, 109 + 8, 97 + 5 (taken: 2048); 2048 tokens, 4096 and 3 x 4096 columns, 3 x 16 ranks 27 + 5, 26 + 5, 28 + 5,
+// 45 + 5 (512); 1000 tokens of five adapters, 2816 and 2056 columns, 24 ranks 10 + 3, 13 + 4, 14 + 4, 14 + 4 (256).
 constexpr int kLoraGradBlocks = 400;
 inline int lora_grad_len(int64_t T, int64_t col_blocks) {
   int i = kLoraGradLens - 1;
