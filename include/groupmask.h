@@ -476,7 +476,8 @@ gm_status gm_tensor_list(float* const* p, const void* const* g, float* const* m,
 /*
  * gm_grad_norm -- norm = sqrt(sum of the squares of every gradient of the
  * list) and coef = min(1, max_norm / norm), one fp32 each (device).  The sum is
- * in fp64 and in a fixed order.  A norm that is not finite gives coef = 0.
+ * in fp64 and in a fixed order.  A norm that is not finite in fp32 gives coef = 0,
+ * whatever max_norm; any other gives coef > 0, at least the least positive fp32 value (2^-149).
  *   max_norm > 0 (infinity: coef is 1); ws: GM_GRAD_NORM_WORKSPACE_BYTES of scratch.
  */
 #define GM_GRAD_NORM_WORKSPACE_BYTES ((size_t)16384)
@@ -487,7 +488,7 @@ gm_status gm_grad_norm(const void* list, size_t list_bytes, float max_norm, floa
  * gm_adamw_list -- one gm_adamw step on every tensor of the list with the gradients coef g
  * (coef: one fp32 (device), or NULL for 1), and the bf16 copies of the new
  * parameters.  The gradients themselves stay as they are.  With coef = 0, as
- * gm_grad_norm gives it for gradients that are not finite (or any coef that is
+ * gm_grad_norm gives it for a norm that is not finite (or any coef that is
  * not positive and finite), nothing is changed.
  * A list without parameters is a no-op.
  */

@@ -143,8 +143,11 @@ __global__ __launch_bounds__(256) void grad_norm_done_kernel(const double* __res
   for (int i = threadIdx.x; i < blocks; i += 256) sum += part[i];
   const double n = sqrt(sum_block(sum));
   if (threadIdx.x == 0) {
-    norm[0] = float(n);
-    coef[0] = !(n < __builtin_huge_val()) ? 0.0f : n > double(max_norm) ? float(double(max_norm) / n) : 1.0f;
+    // 0 stands for a norm that is not finite as it is returned, and for no other: a finite one gets the least positive
+    // fp32 value where its quotient would round to 0.
+    const float f = float(n);
+    norm[0] = f;
+    coef[0] = !(f < __builtin_huge_valf()) ? 0.0f : n > double(max_norm) ? float(fmax(double(max_norm) / n, 0x1p-149)) : 1.0f;
   }
 }
 
