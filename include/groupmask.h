@@ -400,10 +400,11 @@ gm_status gm_adamw(float* p, const float* g, float* m, float* v, int64_t n, doub
  * Rows of tokens without an adapter are base's own in Y and dX, and zero in P.
  * An adapter that no token has gets zero gradients.  Products accumulate in
  * fp32; P, Q, dA and dB stay fp32 (in Y and dX, c P and Q enter with 16 bits of
- * significand; in dA and dB with all 24); Y and dX are rounded once.  Values
- * of a token or of its adapter that are not finite make its rows (and that
- * adapter's gradients) not finite, and no others.  Results do not
- * depend on timing; the order of the batch changes the order of fp32 sums only.
+ * significand; in dA and dB with all 24; below the normal numbers to within
+ * 2^-134); Y and dX are rounded once.  Values of a token or of its adapter that
+ * are not finite make its rows (and that adapter's gradients) not finite, and no
+ * others.  Results do not depend on timing; the order of the batch changes the
+ * order of fp32 sums only.
  *   1 <= T <= 262144; 1 <= n <= 2048; r a multiple of 8 in [8, 128];
  *   1 <= parts <= 4; d_in and every width multiples of 8, d_in and d_out at
  *   most 2^18 each, and (T + 63 min(n + 1, T)) / 64 (d_in + d_out) at most 2^27.

@@ -460,22 +460,23 @@ __device__ __forceinline__ f32x4 sum_splits(const float* p, int splits, int64_t 
 
 // ---------------------------------------------------------------- bf16 terms of fp32 values
 
-// What bf16 term `term` leaves of x.  An infinity is all in the first.
-__device__ __forceinline__ float lora_rest(float x, uint32_t term) {
-  const float h = __uint_as_float(term << 16);
-  return (term & 0x7f80u) == 0x7f80u ? 0.0f : x - h;
-}
-
-// The first N terms of eight values.
+// The first N >= 2 terms of eight values: each term is what the ones before left, rounded.  The first is held to the
+// largest finite bf16 value, which a finite value may round past: what is beyond goes to the second, and so do
+// infinities and NaN.  No later term can.
 template <int N>
 __device__ __forceinline__ void lora_terms(const float (&x)[8], u32x4 (&f)[N]) {
+  constexpr float kMost = 0x1.fep127f;
+  // What the second term leaves: nothing of an infinity.
+  auto rest = [](float v, uint32_t term) { return (term & 0x7f80u) == 0x7f80u ? 0.0f : v - __uint_as_float(term << 16); };
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
     float a = x[2 * p], b = x[2 * p + 1];
+    f[0][p] = pack_bf16x2(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
+    a -= bf16_lo(f[0][p]), b -= bf16_hi(f[0][p]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 1; i < N; ++i) {
       f[i][p] = pack_bf16x2(a, b);
-      a = lora_rest(a, f[i][p] & 0xffffu), b = lora_rest(b, f[i][p] >> 16);
+      a = rest(a, f[i][p] & 0xffffu), b = rest(b, f[i][p] >> 16);
     }
   }
 }
