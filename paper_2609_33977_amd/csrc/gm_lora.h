@@ -82,4 +82,41 @@ inline int lora_splits(int64_t tiles, int ranks, int64_t K) {
   return int(ks < slices ? ks : slices);
 }
 
+// The products with the rank contracted: blocks of 16, 32, 64 or 128 ranks, the columns whose weights are in LDS at a
+// time, and how many blocks run at once (LDS: three per CU at 64 ranks, one beyond; there a sixteenth more, since the
+// tiles are the most that there can be).
+constexpr int lora_up_rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : ranks <= 64 ? 4 : 8; }
+constexpr int lora_up_cols(int rank_tiles) { return rank_tiles <= 2 ? 512 : 256; }
+constexpr int lora_up_resident(int ranks) { return ranks <= 64 ? 768 : 272; }
+
+inline int64_t lora_up_blocks(const int* widths, int parts, int span, int64_t tiles) {
+  int64_t n = 0;
+  for (int p = 0; p < parts; ++p) n += (widths[p] + span - 1) / span;
+  return n * tiles;
+}
+
+// Columns of such a block, 1024 to 256.  Up to 32 ranks, and for dX, narrower ones until there are four blocks per CU to
+// hide latency (4099 tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
+// terms that every block stages count for more, in tiles of few tokens (64 tokens of 32 adapters, 15360
+// columns: 9.0 us with two, 11.4 with four).  Beyond, where staging costs a block
+// about as much as 384 columns, the width whose rounds of blocks cost least: 8192 tokens of one
+// adapter, 4096 columns, 64 ranks, one round of 1024 columns 36 us, two of 512 43; 203 tokens of 40 adapters,
+// 22016 columns, two rounds of 1024 33, three of 512 29.  At 128 ranks, the whole forward with 256 / 512 / 1024
+// columns: 2048 tokens of 4096 columns 30.1, 25.2, 33.1 us (taken: 512); 1024 of 11008 40.1, 38.8, 34.6 (1024).
+// Past 128 ranks (dX of stacked parts) the sums of all rounds are in registers, for the columns in LDS.
+inline int lora_up_span(const int* widths, int parts, int64_t T, int64_t tiles, int ranks, bool dx) {
+  if (ranks > 128) return lora_up_cols(8);
+  int span = 1024;
+  if (dx || ranks <= 32) {
+    const int want = dx || T >= tiles * (kLoraTile / 2) ? 1024 : 512;
+    while (span > 256 && lora_up_blocks(widths, parts, span, tiles) < want) span /= 2;
+    return span;
+  }
+  const int64_t at_once = lora_up_resident(ranks);
+  auto cost = [&](int s) { return (lora_up_blocks(widths, parts, s, tiles) + at_once - 1) / at_once * (s + 384); };
+  for (int s = 512; s >= 256; s /= 2)
+    if (cost(s) < cost(span)) span = s;
+  return span;
+}
+
 }  // namespace gm

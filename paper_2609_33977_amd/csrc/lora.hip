@@ -613,7 +613,7 @@ __device__ __forceinline__ void lora_copy(const LoraUp& a, const LoraPlan& plan,
 
 // Columns whose weights are in LDS at a time.
 template <int RT>
-constexpr int kUpCols = RT <= 2 ? 512 : 256;
+constexpr int kUpCols = lora_up_cols(RT);
 
 // B's chunk of 8 ranks c of row o is at c ^ up_swizzle(o): the rows that eight lanes read at once then lie in
 // different 16-byte columns.
@@ -1020,30 +1020,10 @@ static hipError_t launch_down(const LoraDown& a, const LoraPlan& plan, int tiles
   return hipGetLastError();
 }
 
-// Blocks of 1024 to 256 columns.  Up to 32 ranks, and for dX, narrower ones until there are four blocks per CU to hide
-// latency (4099 tokens of 12 adapters, 11008 columns, 16 ranks: 50 us with two, 45 with four), or two where the
-// terms that every block stages count for more, in tiles of few tokens (64 tokens of 32 adapters, 15360
-// columns: 9.0 us with two, 11.4 with four).  Beyond, where 768 blocks fit the chip at once and staging costs a block
-// about as much as 384 columns, the width whose rounds of blocks cost least: 8192 tokens of one
-// adapter, 4096 columns, 64 ranks, one round of 1024 columns 36 us, two of 512 43; 203 tokens of 40 adapters,
-// 22016 columns, two rounds of 1024 33, three of 512 29.
+// Deals the parts' columns to blocks; returns how many there are.
 template <bool TR>
 static int up_blocks(LoraUp& u, int ranks, int tiles, const LoraPlan& plan) {
-  auto blocks = [&](int span) {
-    int64_t n = 0;
-    for (int p = 0; p < u.parts; ++p) n += (u.width[p] + span - 1) / span;
-    return n * tiles;
-  };
-  u.span = 1024;
-  if (TR || ranks <= 32) {
-    const int want = TR || plan.T >= tiles * (kLoraTile / 2) ? 1024 : 512;
-    while (u.span > 256 && blocks(u.span) < want) u.span /= 2;
-  } else {
-    auto cost = [&](int span) { return (blocks(span) + 767) / 768 * (span + 384); };
-    for (int span = 512; span >= 256; span /= 2)
-      if (cost(span) < cost(u.span)) u.span = span;
-  }
-  if (ranks > 128) u.span = kUpCols<8>;
+  u.span = lora_up_span(u.width, u.parts, plan.T, tiles, ranks, TR);
   for (int p = 0, off = 0; p < u.parts; ++p) {
     u.off[p] = off;
     off += u.width[p];

@@ -1,0 +1,37 @@
+"""How the adapters' kernels divide their work, asked of the library's own rules (gm_lora.h, compiled for the host)."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no host C++ compiler")
+    exe = str(tmp_path_factory.mktemp("lora") / "lora_plan")
+    subprocess.run([cxx, "-std=c++17", "-O1", "-Wall", "-Werror", "-o", exe, os.path.join(HERE, "lora_plan.cpp")], check=True)
+
+    def ask(op, shapes):  # (T, n, d_in, widths, r)
+        text = "".join(f"{op} {T} {n} {d} {r} {len(w)} {' '.join(map(str, w))}\n" for T, n, d, w, r in shapes)
+        out = subprocess.run([exe], input=text, capture_output=True, text=True, check=True).stdout.splitlines()
+        assert len(out) == len(shapes)
+        return out
+
+    return ask
+
+
+def test_forward_blocks_beyond_64_ranks_by_what_runs_at_once(plan):
+    # one block per CU there (99 KB of LDS): the widths that were measured best, with 256, 512 and 1024 columns tried
+    best = [(2048, 1, 512, (4096,), 128, 512), (1024, 1, 512, (11008,), 128, 1024), (4096, 1, 512, (4096,), 72, 1024),
+            (512, 1, 512, (4096,), 128, 256), (64, 32, 512, (4096,), 128, 512), (8192, 1, 512, (11008,), 128, 1024),
+            (203, 40, 512, (4096,) * 3, 96, 1024), (2048, 1, 512, (4096,), 64, 256), (1024, 1, 512, (11008,), 64, 256)]
+    assert [int(g.split("/")[0]) for g in plan("fwd", [b[:5] for b in best])] == [b[5] for b in best]
+
+
+def test_dx_of_more_than_128_ranks_takes_the_columns_in_lds(plan):
+    assert plan("dx", [(4096, 1, 8192, (64,) * 4, 128), (64, 40, 64, (64,) * 3, 64)]) == ["256/256"] * 2
