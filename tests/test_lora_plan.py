@@ -5,6 +5,8 @@ import subprocess
 
 import pytest
 
+import test_gpu_lora_lengths as lengths
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 
 
@@ -35,3 +37,14 @@ def test_forward_blocks_beyond_64_ranks_by_what_runs_at_once(plan):
 
 def test_dx_of_more_than_128_ranks_takes_the_columns_in_lds(plan):
     assert plan("dx", [(4096, 1, 8192, (64,) * 4, 128), (64, 40, 64, (64,) * 3, 64)]) == ["256/256"] * 2
+
+
+def test_gradient_lengths(plan):
+    # what the GPU tests' shapes are named to take
+    shapes = [(sum(counts) + none, n, d, w, r) for counts, n, d, w, r, none, _ in lengths.LENGTHS]
+    assert [int(g) for g in plan("length", shapes)] == [x[6] for x in lengths.LENGTHS]
+    assert {x[6] for x in lengths.LENGTHS} == {512, 1024, 2048}
+    for length in (512, 1024, 2048):
+        counts = [k for x in lengths.LENGTHS if x[6] == length for k in x[0]]
+        assert any(k > length for k in counts) and any(k == length or k % length == 1 for k in counts)
+        assert any(k < length for k in counts)
