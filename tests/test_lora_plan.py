@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 import test_gpu_lora_lengths as lengths
+import test_gpu_lora_wide_blocks as wide
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -48,3 +49,16 @@ def test_gradient_lengths(plan):
         counts = [k for x in lengths.LENGTHS if x[6] == length for k in x[0]]
         assert any(k > length for k in counts) and any(k == length or k % length == 1 for k in counts)
         assert any(k < length for k in counts)
+
+
+def test_widths_of_blocks(plan):
+    shapes = [(sum(wide.TILES) + 3, 40, d, w, r) for d, w, r, _, _ in wide.WIDE]
+    fwd, dx = ([tuple(map(int, g.split("/"))) for g in plan(op, shapes)] for op in ("fwd", "dx"))
+    assert [g[0] for g in fwd] == [x[3] for x in wide.WIDE] and [g[0] for g in dx] == [x[4] for x in wide.WIDE]
+    # every number of rank blocks (16, 32, 64, 128 ranks) has a block, of a part that is as wide, with weights loaded anew
+    anew = {(op, -(-ranks // 16)) for x, f, b in zip(wide.WIDE, fwd, dx)
+            for op, ranks, got, widest in (("fwd", x[2], f, max(x[1])), ("dx", x[2] * len(x[1]), b, x[0]))
+            if got[0] > got[1] and widest > got[1]}
+    for op in ("fwd", "dx"):
+        blocks = {b for o, b in anew if o == op}
+        assert 1 in blocks and 2 in blocks and blocks & {3, 4} and blocks & {5, 6, 7, 8}, (op, blocks)
