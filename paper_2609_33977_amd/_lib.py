@@ -554,9 +554,13 @@ def gm_tensor_list(g, list, p=None, m=None, v=None, p16=None, stream=None) -> No
     g: their gradients, fp32 or bf16 each; p, m, v: parameters and moments (fp32); p16: bf16 copies of the parameters.
     The caller keeps the tensors alive for as long as the list is used."""
     w = "gm_tensor_list"
+    if g is None:
+        raise ValueError(f"{w}: g is required")
     g = tuple(g)
     n = len(g)
     rest = {}
+    if any(t is None for t in g):
+        raise ValueError(f"{w}: g[{[t is None for t in g].index(True)}] is required")
     for what, ts, dtype in (("p", p, torch.float32), ("m", m, torch.float32), ("v", v, torch.float32),
                             ("p16", p16, torch.bfloat16)):
         if ts is not None:
@@ -564,6 +568,8 @@ def gm_tensor_list(g, list, p=None, m=None, v=None, p16=None, stream=None) -> No
             if len(ts) != n:
                 raise ValueError(f"{w}: {what} must hold {n} tensors, got {len(ts)}")
             for t, s in zip(ts, g):
+                if t is None:
+                    raise ValueError(f"{w}: {what} must hold a tensor for every gradient")
                 if t.dtype is not dtype or t.numel() != s.numel():
                     raise ValueError(f"{w}: every {what} must be {dtype} of its gradient's size")
     for t in g:
