@@ -513,7 +513,8 @@ def gm_lora_fwd(X, A, B, scale, plan, base, Y, P=None, ws=None, widths=None, str
 
 def gm_lora_bwd(dY, X, A, B, scale, plan, P, base=None, dX=None, dA=None, dB=None, ws=None, widths=None,
                 stream=None) -> None:
-    """Gradients of the adapters and of their input (see gm_lora_bwd in the header); P, base only as the outputs need."""
+    """Gradients of the adapters and of their input (see gm_lora_bwd in the header); P, base and ws only as the outputs
+    need."""
     w = "gm_lora_bwd"
     T, n, R, d_in, d_out, r, parts = _adapters(w, X, A, B, widths)
     dev = _device()
@@ -529,10 +530,13 @@ def gm_lora_bwd(dY, X, A, B, scale, plan, P, base=None, dX=None, dA=None, dB=Non
     if dB is not None:
         db = _on(w, "dB", dB, _F32, B.shape, dev)
         p = _on(w, "P", P, _F32, (T, R), dev)
+    space, nbytes = None, 0  # needed only if something is asked for
+    if ws is not None or dx or da or db:
+        space, nbytes = _on(w, "ws", ws, _U8, None, dev), ws.numel()
     _check(LIB.gm_lora_bwd(y, ldy, x, ldx, _on(w, "A", A, _BF16, None, dev), _on(w, "B", B, _BF16, None, dev),
                            _on(w, "scale", scale, _F32, (n,), dev), _on(w, "plan", plan, _U8, None, dev), plan.numel(), p,
-                           T, n, d_in, parts, len(parts), r, b, ldb, dx, lddx, da, db, _on(w, "ws", ws, _U8, None, dev),
-                           ws.numel(), _stream(stream)), w)
+                           T, n, d_in, parts, len(parts), r, b, ldb, dx, lddx, da, db, space, nbytes,
+                           _stream(stream)), w)
 
 
 # ---- the optimiser's work over lists of tensors
