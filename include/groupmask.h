@@ -464,7 +464,10 @@ gm_status gm_lora_bwd(const uint16_t* dY, int64_t lddy, const uint16_t* X, int64
  * faster where a tensor's buffers lie alike to 16 bytes (p16: 8), as those do that
  * are aligned to 16 bytes or cut alike from one buffer per role.  The list holds the addresses, not
  * the values: it stays good while the buffers live, and the calls below that
- * take it need it ordered before them on their stream.
+ * take it need it ordered before them on their stream.  Writing one is host work, for buffers that
+ * stay (the check for shared memory sorts 5 n ranges; one launch per 48 tensors), not for every step:
+ * through the Python binding 1.1 ms for 448 tensors with parameters and copies, 0.3 ms
+ * with gradients alone.
  *   1 <= n <= 65536; numel[i] >= 0 (pointers of empty tensors may be NULL).  No
  *   buffer that a step writes may share memory with another buffer of the list
  *   (GM_ERR_VALUE; a parameter twice, say); gradients may share theirs, and count as often.
@@ -477,9 +480,11 @@ gm_status gm_tensor_list(float* const* p, const void* const* g, float* const* m,
 /*
  * gm_grad_norm -- norm = sqrt(sum of the squares of every gradient of the
  * list) and coef = min(1, max_norm / norm), one fp32 each (device).  The sum is
- * in fp64 and in a fixed order.  A norm that is not finite in fp32 gives coef = 0,
+ * in fp64 and in a fixed order, and so is the quotient; both results are rounded once,
+ * but max_norm is fp32 itself (a bound that is not an fp32 value is half a step off at
+ * most, 2^-24 of it, when the caller passes it).  A norm that is not finite in fp32 gives coef = 0,
  * whatever max_norm; any other gives coef > 0, at least the least positive fp32 value (2^-149).
- *   max_norm > 0 (infinity: coef is 1); ws: GM_GRAD_NORM_WORKSPACE_BYTES of scratch.
+ *   max_norm > 0 (infinity: coef is 1 for any finite norm); ws: GM_GRAD_NORM_WORKSPACE_BYTES of scratch.
  */
 #define GM_GRAD_NORM_WORKSPACE_BYTES ((size_t)16384)
 gm_status gm_grad_norm(const void* list, size_t list_bytes, float max_norm, float* norm, float* coef, void* ws,

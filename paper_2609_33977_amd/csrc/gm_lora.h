@@ -70,10 +70,10 @@ inline int lora_grad_len(int64_t T, int64_t col_blocks) {
 // Blocks of 16, 32 or 64 ranks.
 inline int lora_rank_tiles(int ranks) { return ranks <= 16 ? 1 : ranks <= 32 ? 2 : 4; }
 
-// Blocks that share a tile's contraction over K: two blocks per CU (what fits at once at 64 ranks; a
+// Blocks that share a tile's contraction over K: two blocks per CU (what fits at once; a
 // sixteenth more, since the tiles are the most that there can be), at least two and at most one per slice.  8192
-// tokens of 11008 columns, 64 ranks: 51 us with three splits of 128 tiles, 48 with four.  Three blocks per CU, which fit at
-// fewer ranks, gave nothing there (4099 tokens of 4096 columns, 16 ranks: 9.6 and 10.2 us).
+// tokens of 11008 columns, 64 ranks: 51 us with three splits of 128 tiles, 48 with four.  Splits for three blocks per CU
+// gave nothing (4099 tokens of 4096 columns, 16 ranks: 9.1 us with two, 10.1 with three).
 inline int lora_splits(int64_t tiles, int ranks, int64_t K) {
   const int rt = lora_rank_tiles(ranks);
   const int64_t slices = (K + kLoraSlice - 1) / kLoraSlice, chunks = (ranks + 16 * rt - 1) / (16 * rt);
